@@ -316,6 +316,53 @@ int dsattn_quantize_mxfp8_shift(const void* src, const float* shift, void* codes
                                 long long rows, int row_len, long long group_rows,
                                 hipStream_t stream);
 
+/*
+ * Backward pass.  Given the inputs of a forward call, its output o, its LSE and the gradient
+ * dout of o, it writes dq, dk and dv.  With P_ij = exp(S_ij - lse_i) over the kept pairs,
+ * recomputed from q and k, and delta_i = dout_i . o_i:
+ *
+ *   dv_j = sum_i P_ij dout_i            dS_ij = P_ij (dout_i . v_j - delta_i)
+ *   dq_i = scale sum_j dS_ij k_j        dk_j = scale sum_i dS_ij q_i
+ *
+ * Rules: DSATTN_RULE_DENSE; or DSATTN_RULE_MASK with the skip mask mask_in, held fixed --
+ * mask_out of a forward call of any rule with the same tile_q and tile_k (128 or 32; 32, 64 or
+ * 128), whose o and lse_out then belong to it.  The other rules are DSATTN_EUNSUPPORTED: pass
+ * the mask that they wrote.  A skipped pair costs nothing where its neighbours in a 64-row tile
+ * and 128-row block are skipped too, and contributes to no gradient; a row that kept nothing
+ * (lse = -inf) gets dq = 0, a key that no row kept dk = dv = 0.  The output of an MX-FP8 call
+ * has no backward pass here (its LSE is that of the quantised scores).
+ *
+ * All arrays as in the forward pass: q, k, v, o, dout, dq, dk, dv contiguous bf16
+ * [B][H][N][d], 16-byte aligned; lse float [B][H][N], 4-byte aligned.  The outputs must not
+ * overlap any input or each other.  P and dS are rounded to bf16 for the products, which
+ * accumulate in fp32, in a fixed order: repeated calls give the same bits.  Mask: N <= 262144.
+ *
+ * workspace is a caller-owned device buffer of at least dsattn_attn_bwd_workspace_bytes(B, H, N)
+ * bytes, 256-byte aligned, overlapping no other buffer of the call; its contents are
+ * overwritten.  Every buffer must live on the device of `stream` (the current one for the null
+ * stream).
+ */
+typedef struct dsattn_bwd_args {
+  int rule;              /* DSATTN_RULE_DENSE or DSATTN_RULE_MASK */
+  const void* q;
+  const void* k;
+  const void* v;
+  const void* o;
+  const float* lse;
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  int B, H, N, d;
+  float scale;
+  int tile_q, tile_k;    /* of mask_in */
+  hipStream_t stream;
+  const uint8_t* mask_in; /* DSATTN_RULE_MASK only, else ignored */
+} dsattn_bwd_args;
+
+size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N);
+int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_bytes);
+
 /* Message describing the last error on this thread ("" after a successful call). */
 const char* dsattn_last_error(void);
 

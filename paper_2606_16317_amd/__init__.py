@@ -74,6 +74,22 @@ class DsAttnArgs(ctypes.Structure):
     ]
 
 
+class DsAttnBwdArgs(ctypes.Structure):
+    """Mirror of ``dsattn_bwd_args`` in include/dsattn.h."""
+
+    _fields_ = [
+        ("rule", ctypes.c_int),
+        *((name, ctypes.c_void_p) for name in ("q", "k", "v", "o", "lse", "dout", "dq", "dk",
+                                               "dv")),
+        *((name, ctypes.c_int) for name in ("B", "H", "N", "d")),
+        ("scale", ctypes.c_float),
+        ("tile_q", ctypes.c_int),
+        ("tile_k", ctypes.c_int),
+        ("stream", ctypes.c_void_p),
+        ("mask_in", ctypes.c_void_p),
+    ]
+
+
 _FWD_ARGS = [ctypes.c_void_p] * 4 + [ctypes.c_int] * 4 + [ctypes.c_float, ctypes.c_float,
                                                            ctypes.c_int, ctypes.c_int,
                                                            ctypes.c_void_p, ctypes.c_void_p]
@@ -129,6 +145,11 @@ def lib():
         L.dsattn_key_mean_ws.argtypes = [ctypes.c_void_p, ctypes.c_void_p] + [ctypes.c_int] * 3 + [
             ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
         L.dsattn_key_mean_ws.restype = ctypes.c_int
+        L.dsattn_attn_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 3
+        L.dsattn_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.dsattn_attn_bwd.argtypes = [ctypes.POINTER(DsAttnBwdArgs), ctypes.c_void_p,
+                                      ctypes.c_size_t]
+        L.dsattn_attn_bwd.restype = ctypes.c_int
         L.dsattn_last_error.argtypes = []
         L.dsattn_last_error.restype = ctypes.c_char_p
         L.dsattn_version.argtypes = []
@@ -516,6 +537,61 @@ def dsattn_attn_fwd_reordered_noalloc(rule, param, q, k, v, q_index, kv_index, o
     return o
 
 
+def dsattn_attn_bwd_workspace_bytes(B, H, N):
+    return int(lib().dsattn_attn_bwd_workspace_bytes(B, H, N))
+
+
+def _like(name, t, ref):
+    """t, checked to be a contiguous bf16 GPU tensor of ref's shape; a new one for None."""
+    import torch
+
+    if t is None:
+        return torch.empty_like(ref)
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+        raise TypeError(f"{name} must be a bfloat16 tensor")
+    if not t.is_cuda or not t.is_contiguous() or t.shape != ref.shape:
+        raise ValueError(f"{name} must be a contiguous GPU tensor of shape {tuple(ref.shape)}")
+    return t
+
+
+def _scratch(workspace, need, device, stream):
+    """(workspace tensor, address, bytes) of a call that needs `need` bytes."""
+    if workspace is None:
+        workspace = _workspace(max(need, 1), device, stream)
+    elif not workspace.is_cuda or not workspace.is_contiguous():
+        raise ValueError("workspace must be a contiguous GPU tensor")
+    return workspace, workspace.data_ptr(), workspace.numel() * workspace.element_size()
+
+
+def dsattn_attn_bwd(rule, q, k, v, o, lse, do, dq=None, dk=None, dv=None, scale=None,
+                    tile_q=TILE_Q, tile_k=TILE_K, mask_in=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dv) of a forward call from its output ``o``, its ``lse_out`` and the
+    gradient ``do`` of o: RULE_DENSE, or RULE_MASK with the skip mask ``mask_in`` that the call
+    wrote or reused (``mask_out`` of any rule, same tile_q and tile_k), held fixed.
+    ``workspace`` (a uint8 GPU tensor of ``dsattn_attn_bwd_workspace_bytes``) is allocated here,
+    from the pool of the call's stream, when not given."""
+    import torch
+
+    B, H, N, d = _shape(q, k, v, o)
+    if do is None:
+        raise TypeError("do must be a bfloat16 tensor")
+    do = _like("do", do, q)
+    dq, dk, dv = (_like(n, t, q) for n, t in (("dq", dq), ("dk", dk), ("dv", dv)))
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    ls = _ptr(lse, B * H * N, (torch.float32,), "lse")
+    mi = None
+    if mask_in is not None:
+        mi = _ptr(mask_in, B * H * -(-N // max(1, tile_q)) * -(-N // max(1, tile_k)),
+                  (torch.uint8,), "mask_in")
+    workspace, at, size = _scratch(workspace, dsattn_attn_bwd_workspace_bytes(B, H, N), q.device,
+                                   stream)
+    a = DsAttnBwdArgs(rule, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), ls,
+                      do.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), B, H, N, d,
+                      scale, tile_q, tile_k, _stream(stream), mi)
+    _check(lib().dsattn_attn_bwd(ctypes.byref(a), at, size), "dsattn_attn_bwd")
+    return dq, dk, dv
+
+
 __all__ = [
     "HEAD_DIM", "TILE_Q", "TILE_K", "ORDER_ASCENDING", "ORDER_DIAGONAL", "RULE_DENSE", "RULE_BLASST", "RULE_DYNSPARSE_RECALL",
     "RULE_DYNSPARSE_LAMBDA", "RULE_MASK", "DsAttnArgs", "lib", "last_error", "dsattn_lambda_from_recall",
@@ -524,4 +600,5 @@ __all__ = [
     "dsattn_reordered_workspace_bytes", "dsattn_attn_fwd_reordered",
     "dsattn_attn_fwd_reordered_noalloc", "STATIC_SCRATCH_BYTES", "dsattn_quantize_mxfp8",
     "dsattn_attn_fwd_mxfp8", "dsattn_key_mean", "QK_BF16", "QK_MXFP8",
+    "DsAttnBwdArgs", "dsattn_attn_bwd_workspace_bytes", "dsattn_attn_bwd",
 ]

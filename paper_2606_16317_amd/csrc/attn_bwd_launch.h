@@ -1,0 +1,61 @@
+// Internal interface between the C-ABI entry points and the kernels of the backward pass.
+#ifndef DSATTN_ATTN_BWD_LAUNCH_H
+#define DSATTN_ATTN_BWD_LAUNCH_H
+
+#include <hip/hip_runtime_api.h>
+#include <stddef.h>
+#include <stdint.h>
+
+namespace dsattn {
+
+enum { kBwdDense = 0, kBwdMask = 1, kBwdBias = 2 };
+
+// Learned position bias: what the caller gives, and what launch_bias_prepare makes of it.
+struct BiasParams {
+  const float* table;      // [n_buckets][H]
+  const int32_t* bucket;   // [n_dist]: bucket of distance e - (n_q - 1), outside [0, n_buckets): closed
+  int n_buckets;
+  int n_dist;              // n_q + n_k - 1
+  float* by_dist;          // workspace [H][dist_stride]: bias / scale by distance, -inf: closed
+  int32_t* runs;           // workspace [n_runs]: bucket of 32 distances if one, kRunMixed, kRunClosed
+  int dist_stride;         // floats, a multiple of 32
+  int n_runs;              // ceil(n_dist / 32)
+};
+enum { kRunClosed = -1, kRunMixed = -2 };
+
+struct BwdParams {
+  const uint16_t* q;       // bf16 [BH][n_q][128]
+  const uint16_t* k;       // bf16 [BH][n_k][128]
+  const uint16_t* v;
+  const uint16_t* o;
+  const uint16_t* dout;
+  const float* lse;        // [BH][n_q], natural logarithm, -inf: the row saw no key
+  uint16_t* dq;
+  uint16_t* dk;
+  uint16_t* dv;
+  int H, n_q, n_k;
+  float c;                 // scale * log2(e)
+  float scale;
+  // workspace, rows padded to n_rows (a multiple of 64)
+  float* neg_lse2;         // [BH][n_rows]: -lse * log2(e); -inf for rows that saw no key or do not exist
+  float* neg_delta;        // [BH][n_rows]: -(dO . O), then in bias mode -(sum of P dP)
+  int n_rows;
+  // kBwdMask
+  const uint8_t* mask;     // [BH][n_units][n_dec], nonzero: skipped
+  int tile_q, tile_k;
+  int n_units, n_dec;
+  // kBwdBias
+  BiasParams bias;
+  float* dtable;           // [n_buckets][H]
+  float* dtable_part;      // workspace [BH][n_key_groups][n_buckets]
+};
+
+// Rows of a head's padded per-row workspace, and key groups (workgroups of the dk, dv kernel).
+int bwd_padded_rows(int n_q);
+int bwd_key_groups(int n_k);
+
+hipError_t launch_attn_bwd(int mode, const BwdParams& p, int bh, hipStream_t stream);
+
+}  // namespace dsattn
+
+#endif

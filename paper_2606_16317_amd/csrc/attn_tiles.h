@@ -1,0 +1,193 @@
+// Device helpers shared by the backward and the position-bias kernels: MFMA operand types, a
+// swizzled 64 x 128 bf16 tile in LDS that can be read by rows and transposed, and its loader.
+//
+// Register layout of v_mfma_f32_32x32x16_bf16 (lane l, r = l % 32, g = l / 32): A holds row r
+// and B column r with k = 8 g + (0..7); D holds column r and, in register v, row
+// 8 (v / 4) + 4 g + v % 4.  A product X^T = A B^T whose columns are "own" rows (one per lane
+// pair l, l ^ 32) is therefore, rounded to bf16, the B operand of the next product over those
+// register rows: registers 8 s .. 8 s + 7 are k-step s.
+//
+// Tile swizzle: 16-byte chunk c of row i sits in slot c ^ f(i), f(i) = 4 (i % 4) + (i / 4) % 4.
+// f takes 16 values over 16 consecutive rows (row operands: 16 lanes read one chunk of 16 rows)
+// and its upper two bits differ over 4 consecutive rows (transposed reads: 32 lanes read four
+// chunks of 4 rows), so both kinds of read touch every bank once.
+#ifndef DSATTN_ATTN_TILES_H
+#define DSATTN_ATTN_TILES_H
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace dsattn {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int kD = 128;                  // head dimension
+constexpr int kRowBytes = kD * 2;
+constexpr int kTile = 64;                // rows of an LDS tile
+constexpr int kTileElems = kTile * kD;   // 16 KiB
+constexpr int kWaves = 4;
+constexpr int kThreads = kWaves * 64;
+
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ void sched_fence() { __builtin_amdgcn_sched_barrier(0); }
+__device__ __forceinline__ float neg_inf() { return -__builtin_inff(); }
+
+// Sum of a value over the two lanes (l, l ^ 32) of an own row.
+__device__ __forceinline__ float half_sum(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return __builtin_bit_cast(float, (uint32_t)sw[0]) + __builtin_bit_cast(float, (uint32_t)sw[1]);
+}
+
+__device__ __forceinline__ int tile_swz(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
+
+// LDS byte address of p.
+__device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)p; }
+
+// Operand reads take the LDS byte address of a block's first row plus the lane's own part
+// (row_lane, col_lane); what changes from operand to operand is then an XOR with a constant
+// and a constant offset, of which only the XOR takes an instruction and none a register for
+// longer than the read.  here() keeps the compiler from holding all the XORed addresses of a
+// loop in registers instead.
+__device__ __forceinline__ uint32_t row_lane(int r, int g) {
+  return (uint32_t)(r * kRowBytes + ((tile_swz(r) ^ g) << 4));
+}
+__device__ __forceinline__ uint32_t col_lane(int lane) {
+  const int grp = lane >> 4, lg = lane & 15, g = grp >> 1, i = lg >> 2;
+  return (uint32_t)((4 * g + i) * kRowBytes + (i << 6) +
+                    (((2 * (grp & 1) + ((lg & 3) >> 1)) ^ g) << 4) + 8 * (lg & 1));
+}
+__device__ __forceinline__ void here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+// Row operand: rows r of the block, k-step s (columns 16 s + 8 g + 0..7).
+__device__ __forceinline__ bf16x8 row_operand(uint32_t at, int offset, int s) {
+  typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
+  return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)((at ^ (uint32_t)(s << 5)) + offset));
+}
+
+// Transposed operand: columns 32 db + r as rows; k-step s (0..1) of the 32-row block, the rows
+// that registers 8 s .. 8 s + 7 of a D block hold.
+__device__ __forceinline__ bf16x8 col_operand(uint32_t at, int offset, int s, int db) {
+  typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
+  bf16x8 out;
+#pragma unroll
+  for (int c = 0; c < 2; ++c) {
+    const uint32_t x = (at ^ (uint32_t)((db << 6) | (c << 5))) + offset + 8 * (2 * s + c) * kRowBytes;
+    const bf16x4 y = __builtin_bit_cast(
+        bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(uintptr_t)x));
+#pragma unroll
+    for (int i = 0; i < 4; ++i) out[4 * c + i] = y[i];
+  }
+  return out;
+}
+
+__device__ __forceinline__ f32x16 mfma(const bf16x8& a, const bf16x8& b, const f32x16& c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+}
+
+// Buffer resource of `rows` rows of one head: rows past the end read as zeros.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t row_buffer(const uint16_t* base, int rows) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, rows * kRowBytes, 0x00020000);
+}
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t word_buffer(const void* base, int words) {
+  return __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, words * 4, 0x00020000);
+}
+
+// Byte offset, inside a tile, of what lane `lane` of wave w fetches first: wave w copies the
+// 1 KiB blocks (4 rows) u * 4 + w, lane l the slot l % 16 of row l / 16.  f depends on the row
+// modulo 16 only, so one offset serves all four blocks.
+__device__ __forceinline__ uint32_t tile_lane_offset(int w, int lane) {
+  const int row = 4 * w + (lane >> 4);
+  return (uint32_t)(row * kRowBytes + ((lane & 15) ^ tile_swz(row)) * 16);
+}
+
+// Copy rows row0 .. row0 + 63 into an LDS tile, without registers (see the swizzle above).
+// Inline assembly, since the compiler cannot tell which tile such a load writes and would wait
+// for all of them before any LDS read; the caller waits with tiles_ready.  M0 (the LDS base) is
+// saved and restored, with the wait state that an M0 write needs before the load.
+__device__ __forceinline__ void load_tile(uint16_t* tile, __amdgpu_buffer_rsrc_t rs, uint32_t off,
+                                          int row0, int w) {
+  const uint32_t o0 = off + (uint32_t)row0 * kRowBytes;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(tile + w * 512));
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %[sv], m0\n\t"
+      "s_mov_b32 m0, %[l0]\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[o0], %[rs], 0 offen lds\n\t"
+      "s_add_u32 m0, %[l0], 0x1000\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[o1], %[rs], 0 offen lds\n\t"
+      "s_add_u32 m0, %[l0], 0x2000\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[o2], %[rs], 0 offen lds\n\t"
+      "s_add_u32 m0, %[l0], 0x3000\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dwordx4 %[o3], %[rs], 0 offen lds\n\t"
+      "s_mov_b32 m0, %[sv]"
+      : [sv] "=&s"(saved)
+      : [l0] "s"(lds0), [o0] "v"(o0), [o1] "v"(o0 + 4096u), [o2] "v"(o0 + 8192u),
+        [o3] "v"(o0 + 12288u), [rs] "s"(rs)
+      : "memory", "scc");
+}
+
+// Copy 64 words (word0 .. word0 + 63, those outside the buffer as zeros) into LDS.
+__device__ __forceinline__ void load_words(const void* dst, __amdgpu_buffer_rsrc_t rs, int word0,
+                                           int lane) {
+  const uint32_t o0 = (uint32_t)(word0 + lane) * 4u;
+  const uint32_t lds0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)dst);
+  uint32_t saved;
+  asm volatile(
+      "s_mov_b32 %[sv], m0\n\t"
+      "s_mov_b32 m0, %[l0]\n\t"
+      "s_nop 0\n\t"
+      "buffer_load_dword %[o0], %[rs], 0 offen lds\n\t"
+      "s_mov_b32 m0, %[sv]"
+      : [sv] "=&s"(saved)
+      : [l0] "s"(lds0), [o0] "v"(o0), [rs] "s"(rs)
+      : "memory", "scc");
+}
+
+// This wave's loads have arrived and every wave is here: the loaded tiles can be read, and the
+// tiles read before can be overwritten.
+__device__ __forceinline__ void tiles_ready() {
+  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Own-row fragments (B operands, all eight k-steps) of one row of a head; zeros where !valid.
+__device__ __forceinline__ void load_row(bf16x8 (&f)[8], const uint16_t* base, int row, bool valid,
+                                         int g) {
+#pragma unroll
+  for (int s = 0; s < 8; ++s) {
+    const u32x4 x = valid ? *reinterpret_cast<const u32x4*>(base + (size_t)row * kD + 16 * s + 8 * g)
+                          : u32x4{0, 0, 0, 0};
+    f[s] = __builtin_bit_cast(bf16x8, x);
+  }
+}
+
+// Store a^T (four D blocks, columns = own rows) times m as one row of bf16.
+__device__ __forceinline__ void store_row(uint16_t* base, int row, const f32x16 (&a)[4], float m,
+                                          int g) {
+  uint16_t* out = base + (size_t)row * kD;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      bf16x4 h;
+#pragma unroll
+      for (int t = 0; t < 4; ++t) h[t] = (__bf16)(a[db][4 * i + t] * m);
+      *reinterpret_cast<bf16x4*>(out + 32 * db + 8 * i + 4 * g) = h;
+    }
+}
+
+}  // namespace
+}  // namespace dsattn
+
+#endif

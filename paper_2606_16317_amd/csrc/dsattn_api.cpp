@@ -12,6 +12,7 @@
 #include <mutex>
 #include <string>
 
+#include "attn_bwd_launch.h"
 #include "fa_fwd_launch.h"
 #include "quant_launch.h"
 #include "reorder_launch.h"
@@ -710,6 +711,151 @@ size_t dsattn_key_mean_workspace_bytes(int BH, int N, int d) {
 int dsattn_key_mean_ws(const void* k, float* mean_out, int BH, int N, int d, void* workspace,
                        size_t workspace_size, hipStream_t stream) {
   return key_mean(k, mean_out, BH, N, d, workspace, workspace_size, stream);
+}
+
+namespace {
+
+// ---- backward pass --------------------------------------------------------------------
+
+// One buffer of a call: what it is, and what it has to be.
+struct Buffer {
+  const char* name;
+  const void* p;
+  size_t bytes;
+  uintptr_t align;
+  bool written;
+};
+
+// Device that work enqueued on `stream` runs on, or -1.
+int stream_device(hipStream_t stream) {
+  int dev = -1;
+  hipDevice_t d = -1;
+  if (stream != nullptr && hipStreamGetDevice(stream, &d) == hipSuccess) return (int)d;
+  if (hipGetDevice(&dev) != hipSuccess) dev = -1;
+  (void)hipGetLastError();
+  return dev;
+}
+
+// Every buffer is device memory of the stream's device, aligned, and disjoint from every buffer
+// that the call writes.
+int check_buffers(const Buffer* b, int n, hipStream_t stream) {
+  const int dev = stream_device(stream);
+  for (int i = 0; i < n; ++i) {
+    if (b[i].p == nullptr) return fail(DSATTN_EINVAL, "%s must be non-null", b[i].name);
+    hipPointerAttribute_t attr;
+    if (!is_device_pointer(b[i].p) || hipPointerGetAttributes(&attr, b[i].p) != hipSuccess)
+      return fail(DSATTN_EINVAL, "%s is not a device pointer", b[i].name);
+    if (attr.type == hipMemoryTypeDevice && dev >= 0 && attr.device != dev)
+      return fail(DSATTN_EINVAL, "%s is on device %d, the stream on device %d", b[i].name,
+                  attr.device, dev);
+    if (!aligned(b[i].p, b[i].align))
+      return fail(DSATTN_EINVAL, "%s must be %d-byte aligned", b[i].name, (int)b[i].align);
+  }
+  for (int i = 0; i < n; ++i)
+    for (int j = 0; j < n; ++j)
+      if (b[i].written && (!b[j].written || j < i) &&
+          overlap(span(b[i].name, b[i].p, b[i].bytes), span(b[j].name, b[j].p, b[j].bytes)))
+        return fail(DSATTN_EINVAL, "%s must not overlap %s", b[i].name, b[j].name);
+  return DSATTN_OK;
+}
+
+// The workspace's place in the list of buffers, with its size check.
+int check_workspace(const void* workspace, size_t given, size_t need) {
+  if (workspace == nullptr) return fail(DSATTN_EINVAL, "workspace must be non-null");
+  if (given < need)
+    return fail(DSATTN_EINVAL, "workspace too small: %zu bytes given, %zu needed", given, need);
+  return DSATTN_OK;
+}
+
+// Slices of a workspace, in order.
+struct Slices {
+  char* base;
+  size_t used;
+  void* take(size_t bytes) {
+    void* p = base + used;
+    used += round_up(bytes);
+    return p;
+  }
+};
+
+// -lse and -delta of every row, padded.
+size_t bwd_rows_bytes(int B, int H, int n) {
+  return 2 * round_up((size_t)B * (size_t)H * (size_t)dsattn::bwd_padded_rows(n) * sizeof(float));
+}
+
+bool sane_extents(int B, int H, int n) {
+  return B > 0 && H > 0 && n > 0 && (long long)B * H <= 65535 &&
+         (long long)n * kHeadDim * 2 <= INT32_MAX;
+}
+
+}  // namespace
+
+size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N) {
+  return sane_extents(B, H, N) ? bwd_rows_bytes(B, H, N) : 0;
+}
+
+int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_size) {
+  if (args == nullptr) return fail(DSATTN_EINVAL, "args must be non-null");
+  const dsattn_bwd_args& a = *args;
+  const bool masked = a.rule == DSATTN_RULE_MASK;
+  if (a.rule == DSATTN_RULE_BLASST || a.rule == DSATTN_RULE_DYNSPARSE_RECALL ||
+      a.rule == DSATTN_RULE_DYNSPARSE_LAMBDA)
+    return fail(DSATTN_EUNSUPPORTED,
+                "the backward pass takes the dense rule or a skip mask (the rule's mask_out)");
+  if (a.rule != DSATTN_RULE_DENSE && !masked) return fail(DSATTN_EINVAL, "unknown rule %d", a.rule);
+  // The forward call's checks; a mask of 32-key decisions is one that only rules write.
+  dsattn_args f = make_args(DSATTN_RULE_DENSE, 0.f, a.q, a.k, a.v, nullptr, a.B, a.H, a.N, a.d,
+                            a.scale, a.tile_q, a.tile_k, a.stream, nullptr);
+  int rc = check_problem(f);
+  if (rc != DSATTN_OK) return rc;
+  if (masked && (long long)a.N > (long long)kMaxMaskTiles * kTileK)
+    return fail(DSATTN_EUNSUPPORTED, "a skip mask supports N <= %d (got %d)", kMaxMaskTiles * kTileK,
+                a.N);
+  if (empty_problem(f)) {
+    g_last_error.clear();
+    return DSATTN_OK;
+  }
+  const size_t need = bwd_rows_bytes(a.B, a.H, a.N);
+  if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
+  const size_t rows = (size_t)a.B * (size_t)a.H * (size_t)a.N, wide = rows * kHeadDim * 2;
+  const int n_units = (a.N + a.tile_q - 1) / a.tile_q, n_dec = (a.N + a.tile_k - 1) / a.tile_k;
+  const Buffer buffers[] = {
+      {"q", a.q, wide, 16, false},     {"k", a.k, wide, 16, false},
+      {"v", a.v, wide, 16, false},     {"o", a.o, wide, 16, false},
+      {"lse", a.lse, rows * 4, 4, false}, {"dout", a.dout, wide, 16, false},
+      {"dq", a.dq, wide, 16, true},    {"dk", a.dk, wide, 16, true},
+      {"dv", a.dv, wide, 16, true},    {"workspace", workspace, need, kSliceAlign, true},
+      {"mask_in", a.mask_in, (size_t)a.B * a.H * (size_t)n_units * n_dec, 1, false}};
+  if ((rc = check_buffers(buffers, masked ? 11 : 10, a.stream)) != DSATTN_OK) return rc;
+  dsattn::BwdParams p{};
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.k = static_cast<const uint16_t*>(a.k);
+  p.v = static_cast<const uint16_t*>(a.v);
+  p.o = static_cast<const uint16_t*>(a.o);
+  p.dout = static_cast<const uint16_t*>(a.dout);
+  p.lse = a.lse;
+  p.dq = static_cast<uint16_t*>(a.dq);
+  p.dk = static_cast<uint16_t*>(a.dk);
+  p.dv = static_cast<uint16_t*>(a.dv);
+  p.H = a.H;
+  p.n_q = p.n_k = a.N;
+  p.c = (float)((double)a.scale * kLog2e);
+  p.scale = a.scale;
+  Slices ws{static_cast<char*>(workspace), 0};
+  p.n_rows = dsattn::bwd_padded_rows(a.N);
+  const size_t row_floats = (size_t)a.B * (size_t)a.H * (size_t)p.n_rows * sizeof(float);
+  p.neg_lse2 = static_cast<float*>(ws.take(row_floats));
+  p.neg_delta = static_cast<float*>(ws.take(row_floats));
+  p.mask = masked ? a.mask_in : nullptr;
+  p.tile_q = a.tile_q;
+  p.tile_k = a.tile_k;
+  p.n_units = n_units;
+  p.n_dec = n_dec;
+  const hipError_t e = dsattn::launch_attn_bwd(masked ? dsattn::kBwdMask : dsattn::kBwdDense, p,
+                                               a.B * a.H, a.stream);
+  if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+  g_last_error.clear();
+  return DSATTN_OK;
 }
 
 const char* dsattn_last_error(void) { return g_last_error.c_str(); }

@@ -1,0 +1,143 @@
+"""Backward pass: the host side of the C ABI without a GPU -- struct layout, workspace sizes and
+the refusals that need no device pointer -- and the 64-bit reference of the GPU tests against
+autograd and differences."""
+
+import ctypes
+import os
+import re
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+HEADER = os.path.join(ROOT, "include", "dsattn.h")
+
+
+def _lib():
+    import paper_2606_16317_amd as pkg
+
+    if not os.path.exists(pkg.LIB_PATH):
+        pytest.skip("libdsattn.so not built")
+    return pkg
+
+
+def header_fields(struct):
+    text = open(HEADER).read()
+    body = re.search(r"typedef struct %s \{(.*?)\} %s;" % (struct, struct), text, re.S).group(1)
+    body = re.sub(r"/\*.*?\*/", "", body, flags=re.S)
+    names = []
+    for decl in filter(None, (d.strip() for d in body.split(";"))):
+        names += [p.replace("*", " ").split()[-1] for p in decl.split(",")]
+    return names
+
+
+@pytest.mark.parametrize("struct,mirror", [("dsattn_bwd_args", "DsAttnBwdArgs")])
+def test_struct_mirrors(struct, mirror):
+    pkg = _lib()
+    assert header_fields(struct) == [f[0] for f in getattr(pkg, mirror)._fields_]
+
+
+def bwd_args(pkg, **kw):
+    a = pkg.DsAttnBwdArgs(rule=pkg.RULE_DENSE, B=1, H=1, N=64, d=128, scale=0.1, tile_q=128,
+                          tile_k=64)
+    for name, x in kw.items():
+        setattr(a, name, x)
+    return a
+
+
+@pytest.mark.parametrize("kw,rc,message", [
+    (dict(rule=7), -1, "unknown rule"),
+    (dict(rule=1), -2, "dense rule or a skip mask"),
+    (dict(rule=2), -2, "dense rule or a skip mask"),
+    (dict(rule=3), -2, "dense rule or a skip mask"),
+    (dict(N=-1), -1, ">= 0"),
+    (dict(d=64), -2, "head dimension"),
+    (dict(scale=0.0), -1, "scale"),
+    (dict(scale=float("nan")), -1, "scale"),
+    (dict(tile_q=64), -2, "tile shape"),
+    (dict(tile_k=16), -2, "tile shape"),
+    (dict(B=300, H=300), -1, "65535"),
+    (dict(N=8388608), -1, "N must be"),
+    (dict(rule=4, N=262145), -2, "262144"),
+    (dict(), -1, "workspace must be non-null"),
+])
+def test_refusals(kw, rc, message):
+    pkg = _lib()
+    a = bwd_args(pkg, **kw)
+    assert pkg.lib().dsattn_attn_bwd(ctypes.byref(a), None, 0) == rc
+    assert message in pkg.last_error()
+
+
+def test_small_and_host_workspaces_are_refused():
+    pkg = _lib()
+    a = bwd_args(pkg)
+    need = pkg.dsattn_attn_bwd_workspace_bytes(1, 1, 64)
+    host = ctypes.create_string_buffer(2 * need + 256)
+    at = ctypes.addressof(host)
+    assert pkg.lib().dsattn_attn_bwd(ctypes.byref(a), at, need - 1) == -1
+    assert "workspace too small" in pkg.last_error()
+    assert pkg.lib().dsattn_attn_bwd(ctypes.byref(a), at, need) == -1
+    assert "q must be non-null" in pkg.last_error()
+    assert pkg.lib().dsattn_attn_bwd(None, None, 0) == -1
+
+
+@pytest.mark.parametrize("kw", [dict(B=0), dict(H=0), dict(N=0), dict(N=0, rule=4)])
+def test_empty_problems_do_nothing(kw):
+    pkg = _lib()
+    a = bwd_args(pkg, **kw)
+    assert pkg.lib().dsattn_attn_bwd(ctypes.byref(a), None, 0) == 0
+    assert pkg.last_error() == ""
+
+
+def test_workspace_sizes():
+    pkg = _lib()
+    size = pkg.dsattn_attn_bwd_workspace_bytes
+    assert size(0, 1, 64) == size(1, 0, 64) == size(1, 1, 0) == size(-1, 1, 1) == 0
+    assert size(1, 1, 1) == 2 * 256 and size(1, 1, 65) == 2 * 512
+    assert size(2, 40, 32760) == 2 * 80 * 32768 * 4
+    assert size(70000, 1, 1) == 0 and size(1, 1, 1 << 24) == 0
+
+
+@pytest.mark.parametrize("bias,skip", [(False, False), (True, False), (False, True), (True, True)])
+def test_reference_against_autograd(bias, skip):
+    torch = pytest.importorskip("torch")
+    from _grad_ref import Ref
+
+    g = torch.Generator().manual_seed(3)
+    B, H, n_q, n_k = 2, 2, 9, 13
+    q, k, v, do = (torch.randn(B, H, n, 128, generator=g, dtype=torch.float64)
+                   for n in (n_q, n_k, n_k, n_q))
+    b = torch.randn(H, n_q, n_k, generator=g, dtype=torch.float64) if bias else None
+    s = None
+    if skip:
+        s = torch.rand(B, H, n_q, n_k, generator=g) < 0.4
+        s[..., 0] = False
+    leaves = [x.clone().requires_grad_() for x in (q, k, v)] + ([b.clone().requires_grad_()]
+                                                                if bias else [])
+    z = 128 ** -0.5 * leaves[0] @ leaves[1].transpose(-1, -2)
+    if bias:
+        z = z + leaves[3]
+    if skip:
+        z = z.masked_fill(s, float("-inf"))
+    o = torch.softmax(z, -1) @ leaves[2]
+    o.backward(do)
+    ref = Ref(q, k, v, do, bias=b, skip=s)
+    assert torch.allclose(ref.o, o, atol=1e-12)
+    assert torch.allclose(ref.lse, torch.logsumexp(z, -1), atol=1e-12)
+    for x, name in zip(leaves, ("dq", "dk", "dv")):
+        assert torch.allclose(getattr(ref, name), x.grad, atol=1e-11)
+    if bias:
+        assert torch.allclose(ref.ds.sum(0), leaves[3].grad, atol=1e-11)
+
+
+def test_reference_of_rows_with_nothing():
+    torch = pytest.importorskip("torch")
+    from _grad_ref import Ref
+
+    g = torch.Generator().manual_seed(4)
+    q, k, v, do = (torch.randn(1, 1, 5, 128, generator=g, dtype=torch.float64) for _ in range(4))
+    skip = torch.zeros(1, 1, 5, 5, dtype=torch.bool)
+    skip[..., 2, :] = True
+    ref = Ref(q, k, v, do, skip=skip)
+    assert ref.lse[0, 0, 2] == -float("inf") and not ref.o[0, 0, 2].any()
+    assert not ref.dq[0, 0, 2].any() and not ref.ds[0, 0, 2].any()
+    assert all(torch.isfinite(x).all() for x in (ref.dq, ref.dk, ref.dv))
