@@ -363,6 +363,89 @@ typedef struct dsattn_bwd_args {
 size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N);
 int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_bytes);
 
+/*
+ * Attention with a learned relative position bias by buckets:
+ *
+ *   S_ij = scale q_i . k_j + table[bucket[j - i + n_q - 1]][h],   o = softmax(S) v
+ *
+ * over n_q queries and n_k keys, which need not be equally many.  bucket is a device int32
+ * [n_q + n_k - 1] array over all values of j - i, from -(n_q - 1) up, shared by all heads;
+ * table a device float [n_buckets][H].  A bucket outside [0, n_buckets), and a bias of -inf or
+ * below -1e30, closes its pairs: they take no part (with such buckets for later keys the
+ * attention is causal, for far ones it has a window).  A row with no open key gets zeros and an
+ * LSE of -inf.
+ *
+ * q and o are contiguous bf16 [B][H][n_q][d]; k and v are bf16 [B][H][k_rows][d] of which the
+ * first n_k <= k_rows rows of every head are keys (a cache with room; k_rows = n_k otherwise; the
+ * other rows are not read).  With few queries -- one, when a token at a time is added -- the keys
+ * are split over more workgroups and joined in a fixed order.  Extents >= 0, n_q, k_rows <=
+ * 8388607, B*H <= 65535, 1 <= n_buckets <= 512, d = 128; n_k = 0 leaves every row without a key.
+ *
+ * The gradients (dsattn_bias_attn_bwd; k_rows = n_k there) are those of dsattn_attn_bwd, with
+ * the bias in S, and
+ *
+ *   dtable[i][h] = sum over b and the pairs of bucket i of dS          (float [n_buckets][H])
+ *
+ * whose sums are kept in 32 bits up to the parts of 128 keys and joined in 64, in a fixed order.
+ * q, k, v and dout must be finite.
+ *
+ * Memory, alignment, overlap, workspace and device rules are those of dsattn_attn_bwd; table,
+ * bucket, lse_out / lse and dtable are 4-byte aligned.
+ */
+typedef struct dsattn_bias_args {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* table;
+  const int32_t* bucket;
+  int n_buckets;
+  int B, H, n_q, n_k, k_rows, d;
+  float scale;
+  hipStream_t stream;
+  void* o;
+  float* lse_out;        /* float [B][H][n_q]; may be NULL */
+} dsattn_bias_args;
+
+typedef struct dsattn_bias_bwd_args {
+  const void* q;
+  const void* k;
+  const void* v;
+  const float* table;
+  const int32_t* bucket;
+  int n_buckets;
+  int B, H, n_q, n_k, d;
+  float scale;
+  hipStream_t stream;
+  const void* o;
+  const float* lse;
+  const void* dout;
+  void* dq;
+  void* dk;
+  void* dv;
+  float* dtable;
+} dsattn_bias_bwd_args;
+
+size_t dsattn_bias_attn_workspace_bytes(int B, int H, int n_q, int n_k);
+int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t workspace_bytes);
+size_t dsattn_bias_attn_bwd_workspace_bytes(int B, int H, int n_q, int n_k, int n_buckets);
+int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace,
+                         size_t workspace_bytes);
+
+/*
+ * Host function.  Writes the usual bucket map of n_q queries at positions q_first, q_first + 1,
+ * ... and n_k keys at positions 0, 1, ... into bucket_out (host memory, int32 [n_q + n_k - 1]):
+ * with d = key position - query position, P = n_buckets (causal) or n_buckets / 2 (both
+ * directions) and E = max(1, P / 2),
+ *
+ *   f(a) = a for a < E,  min(P - 1, E + floor((P - E) ln(a / E) / ln(max_distance / E))) else
+ *   bucket = f(|d|), and P + f(d) for d > 0, or -1 (closed) for d > 0 when causal.
+ *
+ * n_q, n_k >= 1 and at most 8388607, q_first >= 0 and at most 8388607, n_buckets >= 2,
+ * max_distance > E; DSATTN_EINVAL otherwise, or when bucket_out is NULL or device-only memory.
+ */
+int dsattn_relative_buckets(int n_q, int n_k, int q_first, int n_buckets, int max_distance,
+                            int causal, int32_t* bucket_out);
+
 /* Message describing the last error on this thread ("" after a successful call). */
 const char* dsattn_last_error(void);
 

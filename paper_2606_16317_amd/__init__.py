@@ -90,6 +90,31 @@ class DsAttnBwdArgs(ctypes.Structure):
     ]
 
 
+class DsAttnBiasArgs(ctypes.Structure):
+    """Mirror of ``dsattn_bias_args`` in include/dsattn.h."""
+
+    _fields_ = [
+        *((name, ctypes.c_void_p) for name in ("q", "k", "v", "table", "bucket")),
+        *((name, ctypes.c_int) for name in ("n_buckets", "B", "H", "n_q", "n_k", "k_rows", "d")),
+        ("scale", ctypes.c_float),
+        ("stream", ctypes.c_void_p),
+        ("o", ctypes.c_void_p),
+        ("lse_out", ctypes.c_void_p),
+    ]
+
+
+class DsAttnBiasBwdArgs(ctypes.Structure):
+    """Mirror of ``dsattn_bias_bwd_args`` in include/dsattn.h."""
+
+    _fields_ = [
+        *((name, ctypes.c_void_p) for name in ("q", "k", "v", "table", "bucket")),
+        *((name, ctypes.c_int) for name in ("n_buckets", "B", "H", "n_q", "n_k", "d")),
+        ("scale", ctypes.c_float),
+        *((name, ctypes.c_void_p) for name in ("stream", "o", "lse", "dout", "dq", "dk", "dv",
+                                               "dtable")),
+    ]
+
+
 _FWD_ARGS = [ctypes.c_void_p] * 4 + [ctypes.c_int] * 4 + [ctypes.c_float, ctypes.c_float,
                                                            ctypes.c_int, ctypes.c_int,
                                                            ctypes.c_void_p, ctypes.c_void_p]
@@ -150,6 +175,18 @@ def lib():
         L.dsattn_attn_bwd.argtypes = [ctypes.POINTER(DsAttnBwdArgs), ctypes.c_void_p,
                                       ctypes.c_size_t]
         L.dsattn_attn_bwd.restype = ctypes.c_int
+        L.dsattn_bias_attn_workspace_bytes.argtypes = [ctypes.c_int] * 4
+        L.dsattn_bias_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.dsattn_bias_attn_bwd_workspace_bytes.argtypes = [ctypes.c_int] * 5
+        L.dsattn_bias_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.dsattn_bias_attn_fwd.argtypes = [ctypes.POINTER(DsAttnBiasArgs), ctypes.c_void_p,
+                                           ctypes.c_size_t]
+        L.dsattn_bias_attn_fwd.restype = ctypes.c_int
+        L.dsattn_bias_attn_bwd.argtypes = [ctypes.POINTER(DsAttnBiasBwdArgs), ctypes.c_void_p,
+                                           ctypes.c_size_t]
+        L.dsattn_bias_attn_bwd.restype = ctypes.c_int
+        L.dsattn_relative_buckets.argtypes = [ctypes.c_int] * 6 + [ctypes.c_void_p]
+        L.dsattn_relative_buckets.restype = ctypes.c_int
         L.dsattn_last_error.argtypes = []
         L.dsattn_last_error.restype = ctypes.c_char_p
         L.dsattn_version.argtypes = []
@@ -592,6 +629,105 @@ def dsattn_attn_bwd(rule, q, k, v, o, lse, do, dq=None, dk=None, dv=None, scale=
     return dq, dk, dv
 
 
+def dsattn_relative_buckets(n_q, n_k, n_buckets, max_distance, q_first=0, causal=False):
+    """Bucket map (numpy int32 [n_q + n_k - 1]) of n_q queries at positions q_first, ... and n_k
+    keys at 0, ..., computed by the library's host code: near distances have buckets of their
+    own, far ones share by the logarithm; -1 (closed) for later keys when causal."""
+    import numpy as np
+
+    out = np.empty(max(1, n_q + n_k - 1), dtype=np.int32)
+    rc = lib().dsattn_relative_buckets(n_q, n_k, q_first, n_buckets, max_distance,
+                                       int(bool(causal)), out.ctypes.data)
+    _check(rc, "dsattn_relative_buckets")
+    return out
+
+
+def dsattn_bias_attn_workspace_bytes(B, H, n_q, n_k):
+    return int(lib().dsattn_bias_attn_workspace_bytes(B, H, n_q, n_k))
+
+
+def dsattn_bias_attn_bwd_workspace_bytes(B, H, n_q, n_k, n_buckets):
+    return int(lib().dsattn_bias_attn_bwd_workspace_bytes(B, H, n_q, n_k, n_buckets))
+
+
+def _bias_shape(q, k, v, table, bucket, n_k):
+    """(B, H, n_q, n_k, rows of k, d, n_buckets) of checked arguments."""
+    import torch
+
+    for name, t in (("q", q), ("k", k), ("v", v)):
+        if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
+            raise TypeError(f"{name} must be a bfloat16 tensor")
+        if not t.is_cuda or not t.is_contiguous() or t.dim() != 4:
+            raise ValueError(f"{name} must be a contiguous GPU tensor [B, H, n, d]")
+    if k.shape != v.shape or q.shape[:2] != k.shape[:2] or q.shape[3] != k.shape[3]:
+        raise ValueError("k and v must have the same shape, and q's but for the length")
+    (B, H, n_q, d), rows = (int(x) for x in q.shape), int(k.shape[2])
+    n_k = rows if n_k is None else int(n_k)
+    if not 0 <= n_k <= rows:
+        raise ValueError(f"n_k must lie in [0, {rows}] (got {n_k})")
+    if not isinstance(table, torch.Tensor) or table.dtype != torch.float32:
+        raise TypeError("table must be a float32 tensor")
+    if not table.is_cuda or not table.is_contiguous() or table.dim() != 2 or table.shape[1] != H:
+        raise ValueError(f"table must be a contiguous GPU tensor [n_buckets, {H}]")
+    if not isinstance(bucket, torch.Tensor) or bucket.dtype != torch.int32:
+        raise TypeError("bucket must be an int32 tensor")
+    _ptr(bucket, max(0, n_q + n_k - 1), None, "bucket")
+    return B, H, n_q, n_k, rows, d, int(table.shape[0])
+
+
+def dsattn_bias_attn_fwd(q, k, v, table, bucket, n_k=None, o=None, scale=None, lse_out=None,
+                         workspace=None, stream=None):
+    """Attention with a learned relative position bias: ``table`` (float32 [n_buckets, H]) holds
+    a bias per bucket and head, ``bucket`` (int32 [n_q + n_k - 1]) the bucket of every j - i from
+    -(n_q - 1) up (outside [0, n_buckets): closed).  q is [B, H, n_q, 128]; k and v are [B, H,
+    rows, 128], of which the first ``n_k`` (all by default) are keys.  Returns o; ``lse_out``
+    (float32, B*H*n_q elements) receives the log-sum-exp.  ``workspace`` (a uint8 GPU tensor of
+    ``dsattn_bias_attn_workspace_bytes``) is allocated here when not given."""
+    import torch
+
+    B, H, n_q, n_k, rows, d, n_buckets = _bias_shape(q, k, v, table, bucket, n_k)
+    o = _like("o", o, q)
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    ls = _ptr(lse_out, B * H * n_q, (torch.float32,), "lse_out")
+    workspace, at, size = _scratch(workspace, dsattn_bias_attn_workspace_bytes(B, H, n_q, n_k),
+                                   q.device, stream)
+    a = DsAttnBiasArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                       bucket.data_ptr(), n_buckets, B, H, n_q, n_k, rows, d, scale,
+                       _stream(stream), o.data_ptr(), ls)
+    _check(lib().dsattn_bias_attn_fwd(ctypes.byref(a), at, size), "dsattn_bias_attn_fwd")
+    return o
+
+
+def dsattn_bias_attn_bwd(q, k, v, table, bucket, o, lse, do, dq=None, dk=None, dv=None,
+                         dtable=None, scale=None, workspace=None, stream=None):
+    """Gradients (dq, dk, dv, dtable) of ``dsattn_bias_attn_fwd`` from its output ``o``, its
+    ``lse_out`` and the gradient ``do`` of o; dtable is float32 like the table, summed over the
+    batch.  Every row of k and v is a key here."""
+    import torch
+
+    B, H, n_q, n_k, _, d, n_buckets = _bias_shape(q, k, v, table, bucket, None)
+    for name, t in (("o", o), ("do", do)):
+        if t is None:
+            raise TypeError(f"{name} must be a bfloat16 tensor")
+        _like(name, t, q)
+    dq, dk, dv = (_like(n, t, x) for n, t, x in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    if dtable is None:
+        dtable = torch.empty_like(table)
+    elif dtable.shape != table.shape:
+        raise ValueError(f"dtable must have the table's shape {tuple(table.shape)}")
+    dt = _ptr(dtable, n_buckets * H, (torch.float32,), "dtable")
+    scale = 1.0 / math.sqrt(d) if scale is None else scale
+    ls = _ptr(lse, B * H * n_q, (torch.float32,), "lse")
+    need = dsattn_bias_attn_bwd_workspace_bytes(B, H, n_q, n_k, n_buckets)
+    workspace, at, size = _scratch(workspace, need, q.device, stream)
+    a = DsAttnBiasBwdArgs(q.data_ptr(), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                          bucket.data_ptr(), n_buckets, B, H, n_q, n_k, d, scale,
+                          _stream(stream), o.data_ptr(), ls, do.data_ptr(), dq.data_ptr(),
+                          dk.data_ptr(), dv.data_ptr(), dt)
+    _check(lib().dsattn_bias_attn_bwd(ctypes.byref(a), at, size), "dsattn_bias_attn_bwd")
+    return dq, dk, dv, dtable
+
+
 __all__ = [
     "HEAD_DIM", "TILE_Q", "TILE_K", "ORDER_ASCENDING", "ORDER_DIAGONAL", "RULE_DENSE", "RULE_BLASST", "RULE_DYNSPARSE_RECALL",
     "RULE_DYNSPARSE_LAMBDA", "RULE_MASK", "DsAttnArgs", "lib", "last_error", "dsattn_lambda_from_recall",
@@ -601,4 +737,7 @@ __all__ = [
     "dsattn_attn_fwd_reordered_noalloc", "STATIC_SCRATCH_BYTES", "dsattn_quantize_mxfp8",
     "dsattn_attn_fwd_mxfp8", "dsattn_key_mean", "QK_BF16", "QK_MXFP8",
     "DsAttnBwdArgs", "dsattn_attn_bwd_workspace_bytes", "dsattn_attn_bwd",
+    "DsAttnBiasArgs", "DsAttnBiasBwdArgs", "dsattn_relative_buckets",
+    "dsattn_bias_attn_workspace_bytes", "dsattn_bias_attn_bwd_workspace_bytes",
+    "dsattn_bias_attn_fwd", "dsattn_bias_attn_bwd",
 ]

@@ -29,7 +29,7 @@ SAN_LIB_PATH = os.path.join(PKG_DIR, "libdsattn_san.so")
 ARCH = "gfx950"
 
 SOURCES = ["fa_fwd_kernel.hip", "fa_fwd_side_kernels.hip", "reorder_kernel.hip",
-           "quant_kernel.hip", "attn_bwd_kernel.hip", "dsattn_api.cpp"]
+           "quant_kernel.hip", "attn_bwd_kernel.hip", "bias_fwd_kernel.hip", "dsattn_api.cpp"]
 
 
 def hipcc() -> str:

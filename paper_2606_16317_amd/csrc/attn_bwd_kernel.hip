@@ -104,16 +104,75 @@ __device__ __forceinline__ void build_list(VisitList& list, const BwdParams& p, 
   __syncthreads();
 }
 
+// ---- position bias -----------------------------------------------------------------------
+
+// Distances key - query of a workgroup and a streamed tile: 128 + 64 - 1 of them, in windows of
+// kWindow words that begin with the tile's smallest.
+constexpr int kWindow = 192;
+
+// First and last streamed tile with an open run of distances (first > last: none).  e0(t) is the
+// smallest distance index of tile t.
+struct TileRange {
+  int first, last;
+};
+template <typename F>
+__device__ __forceinline__ void open_tiles(TileRange& range, const BiasParams& b, int n_tiles, F e0) {
+  if (threadIdx.x == 0) {
+    range.first = n_tiles;
+    range.last = -1;
+  }
+  __syncthreads();
+  for (int t = threadIdx.x; t < n_tiles; t += kThreads) {
+    const int e = e0(t);
+    const int j1 = min(b.n_runs - 1, (e + kWindow - 2) >> 5);
+    bool open = false;
+    for (int j = max(0, e >> 5); j <= j1; ++j) open |= b.runs[j] != kRunClosed;
+    if (open) {
+      atomicMin(&range.first, t);
+      atomicMax(&range.last, t);
+    }
+  }
+  __syncthreads();
+}
+
+// The run that a 32 x 32 block lies in (its 63 distances begin at word m of the runs of its
+// tile), or kRunMixed.
+__device__ __forceinline__ int block_run(const int32_t (&runs)[64], int m) {
+  const int x = __builtin_amdgcn_readfirstlane(runs[m]);
+  const int y = __builtin_amdgcn_readfirstlane(runs[m + 1]);
+  const int z = __builtin_amdgcn_readfirstlane(runs[m + 2]);
+  return x == y && y == z ? x : (int)kRunMixed;
+}
+
 // ---- dk, dv ------------------------------------------------------------------------------
 
+// What a workgroup's LDS holds besides tiles.
 struct NoList {};
-template <int MODE>
-struct ListOf {
+struct DkvBias {
+  alignas(16) float win[2][kWindow];       // bias / scale
+  alignas(16) int32_t bucket[2][kWindow];
+  int32_t runs[2][64];
+  float diag[kWaves][2][64];               // sums over a block's distances, per lane half
+  float bins[kWaves][kMaxBuckets];         // sums over buckets
+  float closed[32];                        // -inf, read by lanes whose key does not exist
+  TileRange range;
+};
+struct DqBias {
+  alignas(16) float win[2][kWindow];
+  int32_t runs[2][64];
+  TileRange range;
+};
+template <int MODE, typename BIAS>
+struct SideOf {
   typedef VisitList type;
 };
-template <>
-struct ListOf<kBwdDense> {
+template <typename BIAS>
+struct SideOf<kBwdDense, BIAS> {
   typedef NoList type;
+};
+template <typename BIAS>
+struct SideOf<kBwdBias, BIAS> {
+  typedef BIAS type;
 };
 
 template <int MODE>
@@ -122,8 +181,23 @@ struct DkvSmem {
   alignas(16) uint16_t g[2][kTileElems];   // dO
   alignas(16) float nl[2][kTile];
   alignas(16) float nd[2][kTile];
-  typename ListOf<MODE>::type list;
+  typename SideOf<MODE, DkvBias>::type side;
 };
+
+// The bias of a 32 x 32 block: the run it lies in, its value there, and where this lane reads
+// the single values of a mixed block.
+struct BlockBias {
+  int run;
+  float flat;
+  const float* win;
+};
+
+__device__ __forceinline__ void lds_add(float* p, float x) {
+  __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+}
+
+// Register v's row, 8 (v / 4) + v % 4, counted back from the last one's.
+__device__ __forceinline__ constexpr int back(int v) { return 27 - 8 * (v >> 2) - (v & 3); }
 
 // A workgroup owns 128 keys, a wave 32 of them, and streams the queries in tiles of 64.  Per 32
 // queries: S = Q K^T and dP = dO V^T with keys as columns, so that
@@ -132,14 +206,24 @@ template <int MODE>
 __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int b, uint32_t row_at,
                                           uint32_t col_at, const bf16x8 (&kf)[8],
                                           const bf16x8 (&vf)[8], f32x16 (&dk)[4],
-                                          f32x16 (&dv)[4], float c, int g) {
+                                          f32x16 (&dv)[4], float c, int g, const BlockBias& bias, float& far) {
   constexpr int kG = 2 * kTileElems * 2;   // bytes from the q tiles to the dO tiles
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
   row_at += block;
   col_at += block;
   here(row_at);
   here(col_at);
-  f32x16 s, dp, nd;
+  f32x16 s = f32x16{}, dp, nd;
+  if constexpr (MODE == kBwdBias) {
+    if (bias.run == kRunMixed) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = bias.win[back(v)];
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = bias.flat;
+    }
+  }
+  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.nd[buf][32 * b + 8 * i + 4 * g]);
@@ -161,7 +245,11 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
     s[v] = exp2_fast(fmaf(s[v], c, nl[v >> 2][v & 3]));
     pf[v >> 3][v & 7] = (__bf16)s[v];
   };
-  auto grad = [&](int v) { df[v >> 3][v & 7] = (__bf16)(s[v] * dp[v]); };
+  auto grad = [&](int v) {
+    const float x = s[v] * dp[v];
+    df[v >> 3][v & 7] = (__bf16)x;
+    if constexpr (MODE == kBwdBias) sum += x;
+  };
   constexpr int RK = 3;
   bf16x8 a[RK];
 #pragma unroll
@@ -172,7 +260,7 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
     if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
     const bf16x8& x = a[i % RK];
     if (i < 8)
-      s = mfma(x, kf[i], i == 0 ? f32x16{} : s);
+      s = mfma(x, kf[i], s);
     else if (i < 16)
       dp = mfma(x, vf[i - 8], i == 8 ? nd : dp);
     else if (i < 24)
@@ -190,6 +278,59 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
     }
     sched_fence();
   }
+  // dS in 32 bits, where all of the block is one bucket's
+  if constexpr (MODE == kBwdBias) far += bias.run == kRunMixed ? 0.f : sum;
+}
+
+// dS of a mixed block by distance, in 32 bits: S and dP once more.  (Within dkv_block the 16
+// values would have to outlive the dV products, for which there are no registers; few blocks are
+// mixed.)
+__device__ __forceinline__ void diag_block(const DkvSmem<kBwdBias>& sm, int buf, int b,
+                                           uint32_t row_at, const bf16x8 (&kf)[8],
+                                           const bf16x8 (&vf)[8], float c, int g,
+                                           const float* win, float* diag) {
+  constexpr int kG = 2 * kTileElems * 2;
+  row_at += (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
+  here(row_at);
+  f32x16 s, dp;
+#pragma unroll
+  for (int v = 0; v < 16; ++v) {
+    s[v] = win[back(v)];
+    dp[v] = sm.nd[buf][32 * b + 4 * g + 27 - back(v)];
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    s = mfma(row_operand(row_at, 0, i), kf[i], s);
+    dp = mfma(row_operand(row_at, kG, i), vf[i], dp);
+    sched_fence();
+  }
+#pragma unroll
+  for (int v = 0; v < 16; ++v)
+    lds_add(diag + back(v),
+            exp2_fast(fmaf(s[v], c, sm.nl[buf][32 * b + 4 * g + 27 - back(v)])) * dp[v]);
+}
+
+// Add the sum over one run's elements to its bucket.  (A lane's far is a sum of block sums of 16,
+// the bins take sums of at most 64 blocks: errors grow with the root of each count.)
+__device__ __forceinline__ void flush_far(float* bins, int run, float& far, int lane) {
+  float x = far;
+#pragma unroll
+  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m);
+  if (lane == 0 && run >= 0) lds_add(&bins[run], x);
+  far = 0.f;
+}
+
+// Add a mixed block's sums by distance to their buckets, and clear them.  All of it is one
+// wave's: its LDS accesses run in order.
+__device__ __forceinline__ void flush_diag(float (&diag)[2][64], const int32_t* bucket, float* bins,
+                                           int n_buckets, int lane) {
+  asm volatile("" ::: "memory");
+  const float x = diag[0][lane] + diag[1][lane];
+  const int at = bucket[lane];
+  diag[0][lane] = 0.f;
+  diag[1][lane] = 0.f;
+  if (lane < 63 && (uint32_t)at < (uint32_t)n_buckets) lds_add(&bins[at], x);
+  asm volatile("" ::: "memory");
 }
 
 template <int MODE>
@@ -206,24 +347,42 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   const auto drs = word_buffer(p.neg_delta + (size_t)bh * p.n_rows, p.n_rows);
   const uint32_t off = tile_lane_offset(w, lane);
   const uint32_t row_at = lds_addr(sm.q) + row_lane(r, g), col_at = lds_addr(sm.q) + col_lane(lane);
+  const auto first_distance = [&](int t) { return key0 - (t * kTile + 63) + p.n_q - 1; };
+  const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
+  const auto brs = word_buffer(p.bias.bucket, p.bias.n_dist), rrs = word_buffer(p.bias.runs, p.bias.n_runs);
 
   auto fetch = [&](int buf, int t) {
     load_tile(sm.q[buf], qrs, off, t * kTile, w);
     load_tile(sm.g[buf], grs, off, t * kTile, w);
     if (w == 0) load_words(sm.nl[buf], lrs, t * kTile, lane);
     if (w == 1) load_words(sm.nd[buf], drs, t * kTile, lane);
+    if constexpr (MODE == kBwdBias) {
+      const int e = first_distance(t);
+      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, lane);
+      if (w > 0) load_words(sm.side.bucket[buf] + 64 * (w - 1), brs, e + 64 * (w - 1), lane);
+      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, lane);
+    }
   };
 
-  int count = n_tiles;
-  if constexpr (MODE != kBwdDense) {
-    build_list<MODE, false>(sm.list, p, bh, key0 / 32, n_tiles);
-    count = sm.list.count;
+  int count = n_tiles, first = 0;
+  if constexpr (MODE == kBwdMask) {
+    build_list<MODE, false>(sm.side, p, bh, key0 / 32, n_tiles);
+    count = sm.side.count;
+  }
+  if constexpr (MODE == kBwdBias) {
+    open_tiles(sm.side.range, p.bias, n_tiles, first_distance);
+    first = sm.side.range.first;
+    count = max(0, sm.side.range.last - first + 1);
+    for (int i = tid; i < kWaves * kMaxBuckets; i += kThreads) sm.side.bins[0][i] = 0.f;
+    for (int i = tid; i < kWaves * 128; i += kThreads) sm.side.diag[0][0][i] = 0.f;
+    if (tid < 32) sm.side.closed[tid] = neg_inf();
+    __syncthreads();
   }
   auto tile_at = [&](int i) {
-    if constexpr (MODE == kBwdDense)
-      return i;
+    if constexpr (MODE == kBwdMask)
+      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[i]);
     else
-      return (int)__builtin_amdgcn_readfirstlane(sm.list.tile[i]);
+      return first + i;
   };
 
   if (count > 0) fetch(0, tile_at(0));
@@ -237,21 +396,46 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
 
   // one loop over the 32-row halves: with a loop over tiles around one over their halves the
   // compiler moves all accumulators between the loops
-  uint32_t bits = 0xffffu;
+  const bool own = key0 + 32 * w < p.n_k;   // this wave has a key
+  uint32_t bits = 0xffu;
+  BlockBias bias{};
+  int far_run = kRunClosed;   // the run of the blocks whose sum is in far
+  float far = 0.f;
   for (int i = 0; i < 2 * count; ++i) {
     const int buf = i >> 1 & 1, b = i & 1;
     if (b == 0) {
       tiles_ready();
       if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
-      if constexpr (MODE != kBwdDense) bits = __builtin_amdgcn_readfirstlane(sm.list.bits[i >> 1]);
+      if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
     }
-    const uint32_t keep = bits >> (4 * b + w) & 1u;
-    if (MODE == kBwdDense || keep != 0)
-      dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, g);
+    bool visit = own;
+    if constexpr (MODE == kBwdMask) visit = bits >> (4 * b + w) & 1u;
+    if constexpr (MODE == kBwdBias) {
+      bias.run = block_run(sm.side.runs[buf], 1 + w - b);
+      visit = own && bias.run != kRunClosed;
+      bias.win = key < p.n_k ? &sm.side.win[buf][32 * w + r - 4 * g + 36 - 32 * b] : sm.side.closed;
+      bias.flat = key < p.n_k ? sm.side.win[buf][32 * w - 32 * b + 63] : neg_inf();
+      if (visit && bias.run == kRunMixed) {
+        diag_block(sm, buf, b, row_at, kf, vf, p.c, g, bias.win, &sm.side.diag[w][g][r - 4 * g + 4]);
+        flush_diag(sm.side.diag[w], &sm.side.bucket[buf][32 * w - 32 * b + 32], sm.side.bins[w],
+                   p.bias.n_buckets, lane);
+      } else if (visit && (bias.run != far_run || (i & 63) == 0)) {
+        flush_far(sm.side.bins[w], far_run, far, lane);
+        far_run = bias.run;
+      }
+    }
+    if (visit) dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, g, bias, far);
   }
   if (key < p.n_k) {
     store_row(p.dv + koff, key, dv, 1.f, g);
     store_row(p.dk + koff, key, dk, p.scale, g);
+  }
+  if constexpr (MODE == kBwdBias) {
+    flush_far(sm.side.bins[w], far_run, far, lane);
+    __syncthreads();
+    float* part = p.dtable_part + ((size_t)bh * gridDim.x + blockIdx.x) * p.bias.n_buckets;
+    for (int i = tid; i < p.bias.n_buckets; i += kThreads)
+      part[i] = (sm.side.bins[0][i] + sm.side.bins[1][i]) + (sm.side.bins[2][i] + sm.side.bins[3][i]);
   }
 }
 
@@ -261,34 +445,54 @@ template <int MODE>
 struct DqSmem {
   alignas(16) uint16_t k[2][kTileElems];
   alignas(16) uint16_t v[2][kTileElems];
-  typename ListOf<MODE>::type list;
+  typename SideOf<MODE, DqBias>::type side;
 };
 
 // A workgroup owns 128 queries, a wave 32 of them, and streams the keys in tiles of 64.  Per 32
-// keys: S^T = K Q^T and dP^T = V dO^T with queries as columns, then
-// dQ^T += K^T dS^T.
+// keys: S^T = K Q^T and dP^T = V dO^T with queries as columns, then dQ^T += K^T dS^T.
+//
+// delta: the sum of P dP over the row, which the loop makes on the way, is exact to 32 bits;
+// dO . O is off by the rounding of o, which matters where one key has most of a row, dS being a
+// small difference there.  So dQ is taken with delta' = dO . O and put right at the end,
+// dQ = scale (sum of P (dP - delta') k - (delta - delta') sum of P k), and the dk, dv kernel gets
+// delta.  The fourth product, sum of P k, is its price: without it, dq and dk were off by 4.5e-3
+// of their norm at N = 32760 instead of 2e-3.
+template <int MODE>
 __device__ __forceinline__ void dq_block(int buf, int b, uint32_t row_at, uint32_t col_at,
                                          const bf16x8 (&qf)[8], const bf16x8 (&gf)[8],
-                                         f32x16 (&dq)[4], float nl, float nd, float c, int lim) {
+                                         f32x16 (&dq)[4], f32x16 (&pk)[4], float nl, float nd,
+                                         float c, int g, int left,
+                                         int run, float flat, const float* win, float& delta, float& rest) {
   constexpr int kV = 2 * kTileElems * 2;   // bytes from the k tiles to the v tiles
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
   row_at += block;
   col_at += block;
   here(row_at);
   here(col_at);
-  f32x16 s, dp;
-  bf16x8 df[2];
-  // A operands in the order of their products: S, dP, dQ (eight each)
+  f32x16 s = f32x16{}, dp;
+  if constexpr (MODE == kBwdBias) {
+    if (run == kRunMixed) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = win[27 - back(v)];
+    } else {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[v] = flat;
+    }
+  }
+  float sum = 0.f;
+  bf16x8 pf[2], df[2];
+  // A operands in the order of their products: S, dP, P K, dQ (eight each)
   auto operand = [&](int i) {
     if (i < 16) return row_operand(row_at, i < 8 ? 0 : kV, i & 7);
     return col_operand(col_at, 0, (i & 7) >> 2, i & 3);
   };
-  auto prob = [&](int v) { s[v] = exp2_fast(fmaf(s[v], c, nl)); };
+  auto prob = [&](int v) {
+    s[v] = exp2_fast(fmaf(s[v], c, nl));
+    pf[v >> 3][v & 7] = (__bf16)s[v];
+  };
   auto grad = [&](int v) {
-    float x = s[v] * (dp[v] + nd);
-    // keys past the end: their rows are zeros, but exp2(-lse) may be infinite
-    if (8 * (v >> 2) + (v & 3) >= lim) x = 0.f;
-    df[v >> 3][v & 7] = (__bf16)x;
+    sum = fmaf(s[v], dp[v], sum);
+    df[v >> 3][v & 7] = (__bf16)(s[v] * (dp[v] + nd));
   };
   constexpr int RK = 3;
   bf16x8 a[RK];
@@ -296,31 +500,35 @@ __device__ __forceinline__ void dq_block(int buf, int b, uint32_t row_at, uint32
   for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
   sched_fence();
 #pragma unroll
-  for (int i = 0; i < 24; ++i) {
-    if (i + RK - 1 < 24) a[(i + RK - 1) % RK] = operand(i + RK - 1);
+  for (int i = 0; i < 32; ++i) {
+    if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
     const bf16x8& x = a[i % RK];
     if (i < 8)
-      s = mfma(x, qf[i], i == 0 ? f32x16{} : s);
+      s = mfma(x, qf[i], s);
     else if (i < 16)
       dp = mfma(x, gf[i - 8], i == 8 ? f32x16{} : dp);
+    else if (i < 24)
+      pk[i & 3] = mfma(x, pf[(i & 7) >> 2], pk[i & 3]);
     else
       dq[i & 3] = mfma(x, df[(i & 7) >> 2], dq[i & 3]);
-    if (i >= 9 && i < 16) {
-      prob(2 * (i - 9));
-      prob(2 * (i - 9) + 1);
-    }
-    if (i == 15) {
-      prob(14);
-      prob(15);
+    // keys past the end: their rows are zeros, but exp2(-lse) may be infinite
+    if (i == 8 && left < 32) {
 #pragma unroll
-      for (int v = 0; v < 8; ++v) grad(v);
+      for (int v = 0; v < 16; ++v)
+        if (27 - back(v) + 4 * g >= left) s[v] = neg_inf();
     }
-    if (i >= 16 && i < 20) {
-      grad(8 + 2 * (i - 16));
-      grad(9 + 2 * (i - 16));
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {   // as in dkv_block
+      if (i >= 9 && i < 15) prob((i - 9) * 2 + e);
+      if (i >= 16 && i < 20 && e < 1) prob(i - 4);
+      if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
     sched_fence();
   }
+  // a sum of up to 2^18 block sums: what each addition rounds off is kept beside it
+  const float x = delta + sum, y = x - delta;
+  rest += (delta - (x - y)) + (sum - y);
+  delta = x;
 }
 
 template <int MODE>
@@ -329,30 +537,44 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int bh = blockIdx.y;
-  const int q0 = blockIdx.x * 128;
+  // with a bias that closes later keys, the last queries have the most to do: they go first
+  const int q0 = (MODE == kBwdBias ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x) * 128;
   const int n_tiles = (p.n_k + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
   const uint32_t off = tile_lane_offset(w, lane);
   const uint32_t row_at = lds_addr(sm.k) + row_lane(r, g), col_at = lds_addr(sm.k) + col_lane(lane);
+  const auto first_distance = [&](int t) { return t * kTile - (q0 + 127) + p.n_q - 1; };
+  const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
+  const auto rrs = word_buffer(p.bias.runs, p.bias.n_runs);
   auto fetch = [&](int buf, int t) {
     load_tile(sm.k[buf], krs, off, t * kTile, w);
     load_tile(sm.v[buf], vrs, off, t * kTile, w);
+    if constexpr (MODE == kBwdBias) {
+      const int e = first_distance(t);
+      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, lane);
+      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, lane);
+    }
   };
-  int count = n_tiles;
-  if constexpr (MODE != kBwdDense) {
-    build_list<MODE, true>(sm.list, p, bh, q0 / 32, n_tiles);
-    count = sm.list.count;
+  int count = n_tiles, first = 0;
+  if constexpr (MODE == kBwdMask) {
+    build_list<MODE, true>(sm.side, p, bh, q0 / 32, n_tiles);
+    count = sm.side.count;
+  }
+  if constexpr (MODE == kBwdBias) {
+    open_tiles(sm.side.range, p.bias, n_tiles, first_distance);
+    first = sm.side.range.first;
+    count = max(0, sm.side.range.last - first + 1);
   }
   auto tile_at = [&](int i) {
-    if constexpr (MODE == kBwdDense)
-      return i;
+    if constexpr (MODE == kBwdMask)
+      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[i]);
     else
-      return (int)__builtin_amdgcn_readfirstlane(sm.list.tile[i]);
+      return first + i;
   };
   if (count > 0) fetch(0, tile_at(0));
   bf16x8 qf[8], gf[8];
-  f32x16 dq[4];
+  f32x16 dq[4], pk[4];
   const int row = q0 + w * 32 + r;
   load_row(qf, p.q + qoff, row, row < p.n_q, g);
   load_row(gf, p.dout + qoff, row, row < p.n_q, g);
@@ -360,31 +582,99 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const float nl = row < p.n_q ? p.neg_lse2[at] : neg_inf();
   const float nd = row < p.n_q ? p.neg_delta[at] : 0.f;
 #pragma unroll
-  for (int db = 0; db < 4; ++db) dq[db] = f32x16{};
+  for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
+  const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
   uint32_t bits = 0xffu;
-  int t = 0;
+  int t = 0, run = kRunMixed;
+  float delta = 0.f, rest = 0.f, flat = 0.f;
+  const float* win = nullptr;
   for (int i = 0; i < 2 * count; ++i) {
     const int buf = i >> 1 & 1, b = i & 1;
     if (b == 0) {
       t = tile_at(i >> 1);
       tiles_ready();
       if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
-      if constexpr (MODE != kBwdDense) bits = __builtin_amdgcn_readfirstlane(sm.list.bits[i >> 1]);
+      if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
     }
-    const uint32_t keep = bits >> (4 * b + w) & 1u;
-    if (MODE == kBwdDense || keep != 0)
-      dq_block(buf, b, row_at, col_at, qf, gf, dq, nl, nd, p.c, p.n_k - t * kTile - 32 * b - 4 * g);
+    bool visit = own;
+    if constexpr (MODE == kBwdMask) visit = bits >> (4 * b + w) & 1u;
+    if constexpr (MODE == kBwdBias) {
+      run = block_run(sm.side.runs[buf], 3 + b - w);
+      visit = own && run != kRunClosed;
+      flat = sm.side.win[buf][32 * b - 32 * w + 127];
+      win = &sm.side.win[buf][32 * b + 4 * g - 32 * w - r + 127];
+    }
+    if (visit)
+      dq_block<MODE>(buf, b, row_at, col_at, qf, gf, dq, pk, nl, nd, p.c,
+                     g, p.n_k - t * kTile - 32 * b, run, flat, win, delta, rest);
   }
-  if (row < p.n_q) store_row(p.dq + qoff, row, dq, p.scale, g);
+  const float exact = half_sum(delta + rest), off_by = exact + nd;
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-off_by, pk[db][v], dq[db][v]);
+  if (row < p.n_q) {
+    store_row(p.dq + qoff, row, dq, p.scale, g);
+    if (g == 0) p.neg_delta[at] = -exact;
+  }
 }
 
+// ---- the bias by distance, and the table's gradient -----------------------------------------
+
+// by_dist[h][e] and, from the workgroups of the first head, runs[e / 32].
+__global__ __launch_bounds__(256) void bias_prepare_kernel(BiasParams b, int H, float scale) {
+  const int e = blockIdx.x * 256 + threadIdx.x, h = blockIdx.y;
+  const bool there = e < b.n_dist;
+  int at = there ? b.bucket[e] : -1;
+  if ((uint32_t)at >= (uint32_t)b.n_buckets) at = kRunClosed;
+  if (there) {
+    const float x = at < 0 ? neg_inf() : b.table[(size_t)at * H + h];
+    b.by_dist[(size_t)h * b.dist_stride + e] = x < -1e30f ? neg_inf() : x / scale;
+  }
+  if (h == 0) {
+    const int first = __shfl(at, threadIdx.x & 32);
+    const uint64_t other = __ballot(there && at != first);
+    if ((threadIdx.x & 31) == 0 && there)
+      b.runs[e >> 5] = (uint32_t)(other >> (threadIdx.x & 32)) == 0 ? at : (int)kRunMixed;
+  }
+}
+
+// dtable[i][h]: the parts of all batches and key groups, in 64 bits and a fixed order.  Lane i of
+// every wave takes bucket i, the 16 waves share the parts.
+__global__ __launch_bounds__(1024) void bias_dtable_kernel(BwdParams p, int B, int groups) {
+  __shared__ double sum[16][64];
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = blockIdx.y;
+  const int i = blockIdx.x * 64 + lane, n = p.bias.n_buckets;
+  double x = 0.0;
+  if (i < n)
+    for (int j = w; j < B * groups; j += 16)
+      x += p.dtable_part[((size_t)(j / groups * p.H + h) * groups + j % groups) * n + i];
+  sum[w][lane] = x;
+  __syncthreads();
+  if (w == 0 && i < n) {
+    for (int j = 1; j < 16; ++j) x += sum[j][lane];
+    p.dtable[(size_t)i * p.H + h] = (float)x;
+  }
+}
+
+// (Without queries, keys or batches, which only a bias call passes on, the rest still runs.)
 template <int MODE>
 hipError_t launch_mode(const BwdParams& p, int bh, hipStream_t stream) {
-  hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, bh), dim3(256), 0, stream, p);
-  hipLaunchKernelGGL((bwd_dq_kernel<MODE>), dim3((p.n_q + 127) / 128, bh), dim3(kThreads), 0,
-                     stream, p);
-  hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), dim3((p.n_k + 127) / 128, bh), dim3(kThreads), 0,
-                     stream, p);
+  if (MODE == kBwdBias) {
+    const hipError_t e = launch_bias_prepare(p.bias, p.H, p.scale, stream);
+    if (e != hipSuccess) return e;
+  }
+  if (bh > 0 && p.n_q > 0) {
+    hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, bh), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((bwd_dq_kernel<MODE>), dim3((p.n_q + 127) / 128, bh), dim3(kThreads), 0,
+                       stream, p);
+  }
+  const int groups = bwd_key_groups(p.n_k);
+  if (bh > 0 && groups > 0)
+    hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), dim3(groups, bh), dim3(kThreads), 0, stream, p);
+  if (MODE == kBwdBias)
+    hipLaunchKernelGGL(bias_dtable_kernel, dim3((p.bias.n_buckets + 63) / 64, p.H), dim3(1024), 0,
+                       stream, p, bh / p.H, groups);
   return hipGetLastError();
 }
 
@@ -393,10 +683,18 @@ hipError_t launch_mode(const BwdParams& p, int bh, hipStream_t stream) {
 int bwd_padded_rows(int n_q) { return (n_q + kTile - 1) / kTile * kTile; }
 int bwd_key_groups(int n_k) { return (n_k + 127) / 128; }
 
+hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream) {
+  if (b.n_dist == 0) return hipSuccess;
+  hipLaunchKernelGGL(bias_prepare_kernel, dim3((b.n_dist + 255) / 256, H), dim3(256), 0, stream, b,
+                     H, scale);
+  return hipGetLastError();
+}
+
 hipError_t launch_attn_bwd(int mode, const BwdParams& p, int bh, hipStream_t stream) {
   switch (mode) {
     case kBwdDense: return launch_mode<kBwdDense>(p, bh, stream);
     case kBwdMask: return launch_mode<kBwdMask>(p, bh, stream);
+    case kBwdBias: return launch_mode<kBwdBias>(p, bh, stream);
     default: return hipErrorInvalidValue;
   }
 }

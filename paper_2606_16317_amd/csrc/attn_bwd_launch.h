@@ -22,6 +22,10 @@ struct BiasParams {
   int n_runs;              // ceil(n_dist / 32)
 };
 enum { kRunClosed = -1, kRunMixed = -2 };
+constexpr int kMaxBuckets = 512;   // what the backward pass keeps of them in LDS
+
+// Fill by_dist and runs.
+hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream);
 
 struct BwdParams {
   const uint16_t* q;       // bf16 [BH][n_q][128]

@@ -1,0 +1,333 @@
+// Attention with a learned position bias by buckets, forward pass, for gfx950:
+//
+//   S_ij = scale q_i . k_j + T[bucket(j - i)][h]      O = softmax(S) V      lse = log sum exp S
+//
+// A workgroup owns 128 queries of one head, a wave 32 of them, and streams keys in tiles of 64
+// with a running maximum and sum.  S_{j+1} is computed during step j, under the exponentials of
+// tile j; its row maximum under the P V products.  The bias is laid out by distance beforehand
+// (one value per head and distance).  A 32 x 32 block whose distances share a bucket, as nearly
+// all do when buckets widen with the distance, adds that one number to the row's reference
+// maximum; only mixed blocks read single values, as the first accumulator of S.
+
+#include "attn_tiles.h"
+#include "bias_fwd_launch.h"
+
+#include <algorithm>
+
+namespace dsattn {
+namespace {
+
+constexpr int kWindow = 192;             // distances of 128 queries and 64 keys, and one
+constexpr float kRescaleSlack = 8.0f;    // log2 units
+
+struct FwdSmem {
+  alignas(16) uint16_t k[2][kTileElems];
+  alignas(16) uint16_t v[2][kTileElems];
+  alignas(16) float win[2][kWindow];
+  int32_t runs[2][64];
+  int first, last;
+};
+
+__device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// A query row's softmax so far, in log2 units, and the tile at hand.
+struct RowState {
+  float m_ref;    // reference maximum, -inf before the first open key
+  float l_half;   // this lane's share of the row sum, relative to m_ref
+};
+
+// What a tile's two 32-key blocks add to S c: nothing where single values started S.
+struct TileBias {
+  float flat[2];
+};
+
+// First product of a block's S: onto the single values of a mixed block, or onto zero.
+__device__ __forceinline__ f32x16 first_product(const bf16x8& a, const bf16x8& q, bool mixed,
+                                                const float* win) {
+  if (mixed) {
+    f32x16 s;
+#pragma unroll
+    for (int v = 0; v < 16; ++v) s[v] = win[8 * (v >> 2) + (v & 3)];
+    return mfma(a, q, s);
+  }
+  return mfma(a, q, f32x16{});
+}
+
+__device__ __forceinline__ float block_max(const f32x16& s) {
+  float m = s[0];
+#pragma unroll
+  for (int v = 1; v < 16; ++v) m = maximum(m, s[v]);
+  return m;
+}
+
+// Maximum over the two lanes of a row.
+__device__ __forceinline__ float row_join(float x) {
+  const uint32_t b = __builtin_bit_cast(uint32_t, x);
+  const auto sw = __builtin_amdgcn_permlane32_swap(b, b, false, false);
+  return maximum(__builtin_bit_cast(float, (uint32_t)sw[0]), __builtin_bit_cast(float, (uint32_t)sw[1]));
+}
+
+__device__ __forceinline__ void mask_keys(f32x16 (&s)[2], int lim) {
+#pragma unroll
+  for (int b = 0; b < 2; ++b)
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (32 * b + 8 * (v >> 2) + (v & 3) >= lim) s[b][v] = neg_inf();
+}
+
+template <bool SPLIT>
+__global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) {
+  __shared__ FwdSmem sm;
+  const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
+  const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int bh = blockIdx.y;
+  // with a bias that closes later keys, the last queries have the most to do: they go first
+  const int q0 = (int)(gridDim.x - 1 - blockIdx.x) * 128;
+  const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.k_rows * kD;
+  const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
+  const auto wrs = word_buffer(p.bias.by_dist + (size_t)(bh % p.H) * p.bias.dist_stride, p.bias.n_dist);
+  const auto rrs = word_buffer(p.bias.runs, p.bias.n_runs);
+  const uint32_t off = tile_lane_offset(w, lane);
+  const uint32_t row_at = lds_addr(sm.k) + row_lane(r, g), col_at = lds_addr(sm.v) + col_lane(lane);
+  const auto first_distance = [&](int t) { return t * kTile - (q0 + 127) + p.n_q - 1; };
+
+  // tiles with an open run of distances, and of those this split's share
+  if (tid == 0) {
+    sm.first = 0x7fffffff;
+    sm.last = -1;
+  }
+  __syncthreads();
+  const int n_tiles = (p.n_k + kTile - 1) / kTile;
+  for (int t = tid; t < n_tiles; t += kThreads) {
+    const int e = first_distance(t), j1 = min(p.bias.n_runs - 1, (e + kWindow - 2) >> 5);
+    bool open = false;
+    for (int j = max(0, e >> 5); j <= j1; ++j) open |= p.bias.runs[j] != kRunClosed;
+    if (open) {
+      atomicMin(&sm.first, t);
+      atomicMax(&sm.last, t);
+    }
+  }
+  __syncthreads();
+  int t0 = __builtin_amdgcn_readfirstlane(sm.first);
+  int t1 = __builtin_amdgcn_readfirstlane(sm.last) + 1;   // none open: t1 = 0 < t0
+  if (SPLIT && t0 < t1) {
+    const int share = (t1 - t0 + p.splits - 1) / p.splits;
+    t0 += (int)blockIdx.z * share;
+    t1 = min(t1, t0 + share);
+  }
+
+  auto fetch_k = [&](int buf, int t) {
+    load_tile(sm.k[buf], krs, off, t * kTile, w);
+    const int e = first_distance(t);
+    if (w < 3) load_words(sm.win[buf] + 64 * w, wrs, e + 64 * w, lane);
+    if (w == 3) load_words(sm.runs[buf], rrs, e >> 5, lane);
+  };
+  auto fetch_v = [&](int buf, int t) { load_tile(sm.v[buf], vrs, off, t * kTile, w); };
+
+  const int row = q0 + 32 * w + r;
+  const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
+  f32x16 o[4];
+#pragma unroll
+  for (int db = 0; db < 4; ++db) o[db] = f32x16{};
+  RowState rs{neg_inf(), 0.f};
+
+  if (t0 < t1) {
+    fetch_k(0, t0);
+    fetch_v(0, t0);
+    if (t0 + 1 < t1) fetch_k(1, t0 + 1);
+    bf16x8 qf[8];
+    load_row(qf, p.q + qoff, row, row < p.n_q, g);
+    tiles_ready();
+
+    // The bias of tile t in buffer buf: which blocks are mixed, and what the others add.
+    auto tile_bias = [&](int buf, TileBias& tb, bool (&mixed)[2]) {
+      int run[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) run[j] = __builtin_amdgcn_readfirstlane(sm.runs[buf][3 - w + j]);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        mixed[b] = !(run[b] == run[b + 1] && run[b] == run[b + 2]) || run[b] == kRunMixed;
+        tb.flat[b] = mixed[b] ? 0.f : sm.win[buf][32 * b - 32 * w + 127] * p.c;
+      }
+    };
+    auto win_at = [&](int buf, int b) { return &sm.win[buf][32 * b + 4 * g - 32 * w - r + 127]; };
+
+    f32x16 s[2];
+    TileBias tb, tb_next{};
+    bool mixed[2];
+    float m_hat = neg_inf();
+    if (own) {
+      tile_bias(0, tb, mixed);
+      uint32_t at = row_at;
+      here(at);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int b = 0; b < 2; ++b) {
+          const bf16x8 a = row_operand(at, b * 32 * kRowBytes, i);
+          s[b] = i == 0 ? first_product(a, qf[0], mixed[b], win_at(0, b)) : mfma(a, qf[i], s[b]);
+        }
+      const int lim = p.n_k - t0 * kTile - 4 * g;
+      if (p.n_k - t0 * kTile < kTile) mask_keys(s, lim);
+      m_hat = row_join(maximum(fmaf(block_max(s[0]), p.c, tb.flat[0]),
+                               fmaf(block_max(s[1]), p.c, tb.flat[1])));
+    }
+
+    for (int t = t0; t < t1; ++t) {
+      const int buf = (t - t0) & 1;
+      tiles_ready();
+      if (t + 2 < t1) fetch_k(buf, t + 2);
+      if (t + 1 < t1) fetch_v(buf ^ 1, t + 1);
+      if (!own) continue;
+
+      if (__ballot(m_hat > rs.m_ref + kRescaleSlack) != 0) {
+        const bool need = m_hat > rs.m_ref + kRescaleSlack;
+        const float alpha = need ? exp2_fast(rs.m_ref - m_hat) : 1.f;
+        rs.m_ref = need ? m_hat : rs.m_ref;
+        rs.l_half *= alpha;
+#pragma unroll
+        for (int db = 0; db < 4; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) o[db][v] *= alpha;
+      }
+      const float base = rs.m_ref == neg_inf() ? 0.f : -rs.m_ref;
+      const float add[2] = {base + tb.flat[0], base + tb.flat[1]};
+
+      // past the last tile these read what an earlier one left, and the results go unused
+      tile_bias(buf ^ 1, tb_next, mixed);
+      uint32_t ka = row_at + (uint32_t)((buf ^ 1) * kTileElems * 2);
+      uint32_t va = col_at + (uint32_t)(buf * kTileElems * 2);
+      here(ka);
+      here(va);
+      // operands in the order of their products: 16 of S (key blocks alternating), 16 of P V
+      auto operand = [&](int i) {
+        if (i < 16) return row_operand(ka, (i & 1) * 32 * kRowBytes, i >> 1);
+        return col_operand(va, ((i - 16) >> 3) * 32 * kRowBytes, ((i - 16) >> 2) & 1, i & 3);
+      };
+      f32x16 sn[2];
+      float xs[32];
+      bf16x8 pf[4];
+      auto prob = [&](int e) {
+        const int b = e >> 4, v = e & 15;
+        const float x = exp2_fast(fmaf(s[b][v], p.c, add[b]));
+        xs[e] = x;
+        pf[e >> 3][e & 7] = (__bf16)x;
+      };
+      constexpr int RK = 3;
+      bf16x8 a[RK];
+#pragma unroll
+      for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
+      float mb[2] = {neg_inf(), neg_inf()};
+      sched_fence();
+#pragma unroll
+      for (int i = 0; i < 32; ++i) {
+        if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
+        const bf16x8& x = a[i % RK];
+        if (i < 2)
+          sn[i] = first_product(x, qf[0], mixed[i], win_at(buf ^ 1, i));
+        else if (i < 16)
+          sn[i & 1] = mfma(x, qf[i >> 1], sn[i & 1]);
+        else
+          o[i & 3] = mfma(x, pf[(i - 16) >> 2], o[i & 3]);
+        // two exponentials under each of the first eight products, one under the next sixteen
+        if (i < 8) {
+          prob(2 * i);
+          prob(2 * i + 1);
+        } else if (i < 24) {
+          prob(i + 8);
+        } else {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const int j = 4 * (i - 24) + e;
+            mb[j >> 4] = maximum(mb[j >> 4], sn[j >> 4][j & 15]);
+          }
+        }
+        sched_fence();
+      }
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 32; ++e) sum += xs[e];
+      rs.l_half += sum;
+      const int left = p.n_k - (t + 1) * kTile;
+      if (left < kTile) {   // the last tile is next: its maximum again, over the keys it has
+        mask_keys(sn, left - 4 * g);
+        mb[0] = block_max(sn[0]);
+        mb[1] = block_max(sn[1]);
+      }
+      m_hat = row_join(maximum(fmaf(mb[0], p.c, tb_next.flat[0]), fmaf(mb[1], p.c, tb_next.flat[1])));
+      tb = tb_next;
+      s[0] = sn[0];
+      s[1] = sn[1];
+    }
+  }
+
+  if (row >= p.n_q) return;
+  const float l = half_sum(rs.l_half);
+  const size_t at = (size_t)bh * p.n_q + row;
+  if constexpr (SPLIT) {
+    const size_t part = (size_t)blockIdx.z * gridDim.y * p.n_q + at;
+    float* out = p.part_o + part * kD;
+#pragma unroll
+    for (int db = 0; db < 4; ++db)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(out + 32 * db + 8 * i + 4 * g) =
+            f32x4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+    if (g == 0) {
+      p.part_ml[2 * part] = rs.m_ref;
+      p.part_ml[2 * part + 1] = l;
+    }
+  } else {
+    store_row(p.o + qoff, row, o, l > 0.f ? 1.f / l : 0.f, g);
+    if (g == 0 && p.lse != nullptr)
+      p.lse[at] = l > 0.f ? (rs.m_ref + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
+  }
+}
+
+// Join the splits of a row: one wave a row, two columns a lane.
+__global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p, int rows) {
+  const int row = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  float m = neg_inf();
+  for (int i = 0; i < p.splits; ++i) m = fmaxf(m, p.part_ml[2 * ((size_t)i * rows + row)]);
+  float l = 0.f, x = 0.f, y = 0.f;
+  if (m > neg_inf())
+    for (int i = 0; i < p.splits; ++i) {
+      const size_t at = (size_t)i * rows + row;
+      const float f = exp2_fast(p.part_ml[2 * at] - m);
+      l = fmaf(f, p.part_ml[2 * at + 1], l);
+      const float2 z = *reinterpret_cast<const float2*>(p.part_o + at * kD + 2 * lane);
+      x = fmaf(f, z.x, x);
+      y = fmaf(f, z.y, y);
+    }
+  const float inv = l > 0.f ? 1.f / l : 0.f;
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  *reinterpret_cast<bf16x2*>(p.o + (size_t)row * kD + 2 * lane) = bf16x2{(__bf16)(x * inv), (__bf16)(y * inv)};
+  if (lane == 0 && p.lse != nullptr)
+    p.lse[row] = l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
+}
+
+}  // namespace
+
+int bias_fwd_splits(int bh, int n_q, int n_k) {
+  const long long groups = (long long)bh * ((n_q + 127) / 128);
+  const int tiles = (n_k + kTile - 1) / kTile;
+  if (groups >= 512) return 1;
+  return (int)std::min<long long>(std::max(1, tiles / 4), (1024 + groups - 1) / groups);
+}
+
+hipError_t launch_bias_fwd(const BiasFwdParams& p, int bh, hipStream_t stream) {
+  const hipError_t e = launch_bias_prepare(p.bias, p.H, p.scale, stream);
+  if (e != hipSuccess) return e;
+  const dim3 grid((p.n_q + 127) / 128, bh, p.splits);
+  if (p.splits == 1) {
+    hipLaunchKernelGGL((bias_fwd_kernel<false>), grid, dim3(kThreads), 0, stream, p);
+  } else {
+    const int rows = bh * p.n_q;
+    hipLaunchKernelGGL((bias_fwd_kernel<true>), grid, dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL(bias_join_kernel, dim3((rows + 3) / 4), dim3(256), 0, stream, p, rows);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace dsattn

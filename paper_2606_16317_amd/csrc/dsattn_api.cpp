@@ -13,6 +13,7 @@
 #include <string>
 
 #include "attn_bwd_launch.h"
+#include "bias_fwd_launch.h"
 #include "fa_fwd_launch.h"
 #include "quant_launch.h"
 #include "reorder_launch.h"
@@ -726,6 +727,15 @@ struct Buffer {
   bool written;
 };
 
+// The buffers of a call.
+struct Buffers {
+  Buffer b[16];
+  int n = 0;
+  void add(const char* name, const void* p, size_t bytes, uintptr_t align, bool written) {
+    b[n++] = Buffer{name, p, bytes, align, written};
+  }
+};
+
 // Device that work enqueued on `stream` runs on, or -1.
 int stream_device(hipStream_t stream) {
   int dev = -1;
@@ -819,14 +829,19 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t rows = (size_t)a.B * (size_t)a.H * (size_t)a.N, wide = rows * kHeadDim * 2;
   const int n_units = (a.N + a.tile_q - 1) / a.tile_q, n_dec = (a.N + a.tile_k - 1) / a.tile_k;
-  const Buffer buffers[] = {
-      {"q", a.q, wide, 16, false},     {"k", a.k, wide, 16, false},
-      {"v", a.v, wide, 16, false},     {"o", a.o, wide, 16, false},
-      {"lse", a.lse, rows * 4, 4, false}, {"dout", a.dout, wide, 16, false},
-      {"dq", a.dq, wide, 16, true},    {"dk", a.dk, wide, 16, true},
-      {"dv", a.dv, wide, 16, true},    {"workspace", workspace, need, kSliceAlign, true},
-      {"mask_in", a.mask_in, (size_t)a.B * a.H * (size_t)n_units * n_dec, 1, false}};
-  if ((rc = check_buffers(buffers, masked ? 11 : 10, a.stream)) != DSATTN_OK) return rc;
+  Buffers bufs;
+  bufs.add("q", a.q, wide, 16, false);
+  bufs.add("k", a.k, wide, 16, false);
+  bufs.add("v", a.v, wide, 16, false);
+  bufs.add("o", a.o, wide, 16, false);
+  bufs.add("lse", a.lse, rows * 4, 4, false);
+  bufs.add("dout", a.dout, wide, 16, false);
+  bufs.add("dq", a.dq, wide, 16, true);
+  bufs.add("dk", a.dk, wide, 16, true);
+  bufs.add("dv", a.dv, wide, 16, true);
+  bufs.add("workspace", workspace, need, kSliceAlign, true);
+  if (masked) bufs.add("mask_in", a.mask_in, (size_t)a.B * a.H * (size_t)n_units * n_dec, 1, false);
+  if ((rc = check_buffers(bufs.b, bufs.n, a.stream)) != DSATTN_OK) return rc;
   dsattn::BwdParams p{};
   p.q = static_cast<const uint16_t*>(a.q);
   p.k = static_cast<const uint16_t*>(a.k);
@@ -854,6 +869,236 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   const hipError_t e = dsattn::launch_attn_bwd(masked ? dsattn::kBwdMask : dsattn::kBwdDense, p,
                                                a.B * a.H, a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+  g_last_error.clear();
+  return DSATTN_OK;
+}
+
+namespace {
+
+// ---- position bias --------------------------------------------------------------------
+
+// Extents, scale and head dimension of a problem with a position bias.
+int check_bias_problem(int B, int H, int n_q, int n_k, int k_rows, int d, int n_buckets, float scale) {
+  if (B < 0 || H < 0 || n_q < 0 || n_k < 0) return fail(DSATTN_EINVAL, "B, H, n_q and n_k must be >= 0");
+  if (k_rows < n_k) return fail(DSATTN_EINVAL, "k_rows must be >= n_k (got %d and %d)", k_rows, n_k);
+  if (!(scale > 0.f) || !std::isfinite(scale))
+    return fail(DSATTN_EINVAL, "scale must be finite and > 0 (got %g)", (double)scale);
+  if (d != kHeadDim)
+    return fail(DSATTN_EUNSUPPORTED, "head dimension %d is not supported (only 128)", d);
+  if (n_buckets < 1 || n_buckets > dsattn::kMaxBuckets)
+    return fail(DSATTN_EUNSUPPORTED, "n_buckets must lie in [1, %d] (got %d)", dsattn::kMaxBuckets,
+                n_buckets);
+  if ((long long)B * H > 65535) return fail(DSATTN_EINVAL, "B*H must be <= 65535 (got %lld)", (long long)B * H);
+  if ((long long)n_q * kHeadDim * 2 > INT32_MAX || (long long)k_rows * kHeadDim * 2 > INT32_MAX)
+    return fail(DSATTN_EINVAL, "n_q and k_rows must be <= %d", (int)(INT32_MAX / (kHeadDim * 2)));
+  if (((long long)n_q + k_rows) * kHeadDim * B * H > (1LL << 40))
+    return fail(DSATTN_EINVAL, "problem too large");
+  return DSATTN_OK;
+}
+
+// Distances of a problem, and the floats per head and words of their layout.
+int bias_dist(int n_q, int n_k) { return n_q > 0 && n_k > 0 ? n_q + n_k - 1 : 0; }
+int bias_stride(int n_q, int n_k) { return (bias_dist(n_q, n_k) + 63) / 64 * 64; }
+int bias_runs(int n_q, int n_k) { return (bias_dist(n_q, n_k) + 31) / 32; }
+
+size_t bias_layout_bytes(int H, int n_q, int n_k) {
+  return round_up((size_t)H * (size_t)bias_stride(n_q, n_k) * sizeof(float)) +
+         round_up((size_t)bias_runs(n_q, n_k) * sizeof(int32_t));
+}
+
+dsattn::BiasParams bias_params(const float* table, const int32_t* bucket, int n_buckets, int H,
+                               int n_q, int n_k, Slices& ws) {
+  dsattn::BiasParams b{};
+  b.table = table;
+  b.bucket = bucket;
+  b.n_buckets = n_buckets;
+  b.n_dist = bias_dist(n_q, n_k);
+  b.dist_stride = bias_stride(n_q, n_k);
+  b.n_runs = bias_runs(n_q, n_k);
+  b.by_dist = static_cast<float*>(ws.take((size_t)H * (size_t)b.dist_stride * sizeof(float)));
+  b.runs = static_cast<int32_t*>(ws.take((size_t)b.n_runs * sizeof(int32_t)));
+  return b;
+}
+
+size_t bias_fwd_bytes(int B, int H, int n_q, int n_k) {
+  const size_t splits = (size_t)dsattn::bias_fwd_splits(B * H, n_q, n_k);
+  const size_t rows = splits == 1 ? 0 : splits * (size_t)B * (size_t)H * (size_t)n_q;
+  return bias_layout_bytes(H, n_q, n_k) + round_up(rows * kHeadDim * sizeof(float)) +
+         round_up(rows * 2 * sizeof(float));
+}
+
+size_t bias_bwd_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
+  const size_t parts = (size_t)B * (size_t)H * (size_t)dsattn::bwd_key_groups(n_k);
+  return bias_layout_bytes(H, n_q, n_k) + bwd_rows_bytes(B, H, n_q) +
+         round_up(parts * (size_t)n_buckets * sizeof(float));
+}
+
+// A workspace is never empty, so that it can always be a buffer of the call.
+size_t at_least_one(size_t bytes) { return bytes > 0 ? bytes : kSliceAlign; }
+
+}  // namespace
+
+size_t dsattn_bias_attn_workspace_bytes(int B, int H, int n_q, int n_k) {
+  if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, 1, 1.f) != DSATTN_OK) return 0;
+  return B == 0 || H == 0 || n_q == 0 ? 0 : at_least_one(bias_fwd_bytes(B, H, n_q, n_k));
+}
+
+size_t dsattn_bias_attn_bwd_workspace_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
+  if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, n_buckets, 1.f) != DSATTN_OK) return 0;
+  return H == 0 ? 0 : at_least_one(bias_bwd_bytes(B, H, n_q, n_k, n_buckets));
+}
+
+int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t workspace_size) {
+  if (args == nullptr) return fail(DSATTN_EINVAL, "args must be non-null");
+  const dsattn_bias_args& a = *args;
+  int rc = check_bias_problem(a.B, a.H, a.n_q, a.n_k, a.k_rows, a.d, a.n_buckets, a.scale);
+  if (rc != DSATTN_OK) return rc;
+  const size_t bh = (size_t)a.B * (size_t)a.H;
+  if (bh == 0 || a.n_q == 0) {
+    g_last_error.clear();
+    return DSATTN_OK;
+  }
+  const size_t need = at_least_one(bias_fwd_bytes(a.B, a.H, a.n_q, a.n_k));
+  if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
+  const size_t wide = kHeadDim * 2;
+  Buffers bufs;
+  bufs.add("q", a.q, bh * a.n_q * wide, 16, false);
+  bufs.add("o", a.o, bh * a.n_q * wide, 16, true);
+  bufs.add("workspace", workspace, need, kSliceAlign, true);
+  if (a.lse_out != nullptr) bufs.add("lse_out", a.lse_out, bh * a.n_q * 4, 4, true);
+  if (a.n_k > 0) {
+    bufs.add("k", a.k, bh * a.k_rows * wide, 16, false);
+    bufs.add("v", a.v, bh * a.k_rows * wide, 16, false);
+    bufs.add("table", a.table, (size_t)a.n_buckets * a.H * 4, 4, false);
+    bufs.add("bucket", a.bucket, (size_t)bias_dist(a.n_q, a.n_k) * 4, 4, false);
+  }
+  if ((rc = check_buffers(bufs.b, bufs.n, a.stream)) != DSATTN_OK) return rc;
+  dsattn::BiasFwdParams p{};
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.k = static_cast<const uint16_t*>(a.k);
+  p.v = static_cast<const uint16_t*>(a.v);
+  p.o = static_cast<uint16_t*>(a.o);
+  p.lse = a.lse_out;
+  p.H = a.H;
+  p.n_q = a.n_q;
+  p.n_k = a.n_k;
+  p.k_rows = a.k_rows;
+  p.c = (float)((double)a.scale * kLog2e);
+  p.scale = a.scale;
+  Slices ws{static_cast<char*>(workspace), 0};
+  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
+  p.splits = dsattn::bias_fwd_splits((int)bh, a.n_q, a.n_k);
+  if (p.splits > 1) {
+    const size_t rows = (size_t)p.splits * bh * (size_t)a.n_q;
+    p.part_o = static_cast<float*>(ws.take(rows * kHeadDim * sizeof(float)));
+    p.part_ml = static_cast<float*>(ws.take(rows * 2 * sizeof(float)));
+  }
+  const hipError_t e = dsattn::launch_bias_fwd(p, (int)bh, a.stream);
+  if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+  g_last_error.clear();
+  return DSATTN_OK;
+}
+
+int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size_t workspace_size) {
+  if (args == nullptr) return fail(DSATTN_EINVAL, "args must be non-null");
+  const dsattn_bias_bwd_args& a = *args;
+  int rc = check_bias_problem(a.B, a.H, a.n_q, a.n_k, a.n_k, a.d, a.n_buckets, a.scale);
+  if (rc != DSATTN_OK) return rc;
+  if (a.H == 0) {
+    g_last_error.clear();
+    return DSATTN_OK;
+  }
+  const size_t bh = (size_t)a.B * (size_t)a.H;
+  const size_t need = at_least_one(bias_bwd_bytes(a.B, a.H, a.n_q, a.n_k, a.n_buckets));
+  if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
+  // Without queries the table, dk and dv still get their zeros, without keys dq.
+  const size_t wide = kHeadDim * 2, q_rows = bh * (size_t)a.n_q, k_rows = bh * (size_t)a.n_k;
+  Buffers bufs;
+  bufs.add("dtable", a.dtable, (size_t)a.n_buckets * a.H * 4, 4, true);
+  bufs.add("workspace", workspace, need, kSliceAlign, true);
+  if (q_rows > 0) {
+    bufs.add("q", a.q, q_rows * wide, 16, false);
+    bufs.add("o", a.o, q_rows * wide, 16, false);
+    bufs.add("lse", a.lse, q_rows * 4, 4, false);
+    bufs.add("dout", a.dout, q_rows * wide, 16, false);
+    bufs.add("dq", a.dq, q_rows * wide, 16, true);
+  }
+  if (k_rows > 0) {
+    bufs.add("k", a.k, k_rows * wide, 16, false);
+    bufs.add("v", a.v, k_rows * wide, 16, false);
+    bufs.add("dk", a.dk, k_rows * wide, 16, true);
+    bufs.add("dv", a.dv, k_rows * wide, 16, true);
+  }
+  if (q_rows > 0 && k_rows > 0) {
+    bufs.add("table", a.table, (size_t)a.n_buckets * a.H * 4, 4, false);
+    bufs.add("bucket", a.bucket, (size_t)bias_dist(a.n_q, a.n_k) * 4, 4, false);
+  }
+  if ((rc = check_buffers(bufs.b, bufs.n, a.stream)) != DSATTN_OK) return rc;
+  dsattn::BwdParams p{};
+  p.q = static_cast<const uint16_t*>(a.q);
+  p.k = static_cast<const uint16_t*>(a.k);
+  p.v = static_cast<const uint16_t*>(a.v);
+  p.o = static_cast<const uint16_t*>(a.o);
+  p.dout = static_cast<const uint16_t*>(a.dout);
+  p.lse = a.lse;
+  p.dq = static_cast<uint16_t*>(a.dq);
+  p.dk = static_cast<uint16_t*>(a.dk);
+  p.dv = static_cast<uint16_t*>(a.dv);
+  p.H = a.H;
+  p.n_q = a.n_q;
+  p.n_k = a.n_k;
+  p.c = (float)((double)a.scale * kLog2e);
+  p.scale = a.scale;
+  Slices ws{static_cast<char*>(workspace), 0};
+  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
+  p.n_rows = dsattn::bwd_padded_rows(a.n_q);
+  p.neg_lse2 = static_cast<float*>(ws.take(bh * (size_t)p.n_rows * sizeof(float)));
+  p.neg_delta = static_cast<float*>(ws.take(bh * (size_t)p.n_rows * sizeof(float)));
+  p.dtable = a.dtable;
+  p.dtable_part = static_cast<float*>(
+      ws.take(bh * (size_t)dsattn::bwd_key_groups(a.n_k) * (size_t)a.n_buckets * sizeof(float)));
+  const hipError_t e = dsattn::launch_attn_bwd(dsattn::kBwdBias, p, (int)bh, a.stream);
+  if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
+  g_last_error.clear();
+  return DSATTN_OK;
+}
+
+int dsattn_relative_buckets(int n_q, int n_k, int q_first, int n_buckets, int max_distance,
+                            int causal, int32_t* bucket_out) {
+  constexpr int kMost = INT32_MAX / (kHeadDim * 2);
+  if (n_q < 1 || n_k < 1 || n_q > kMost || n_k > kMost)
+    return fail(DSATTN_EINVAL, "n_q and n_k must lie in [1, %d]", kMost);
+  if (q_first < 0 || q_first > kMost) return fail(DSATTN_EINVAL, "q_first must lie in [0, %d]", kMost);
+  if (n_buckets < 2) return fail(DSATTN_EINVAL, "n_buckets must be >= 2 (got %d)", n_buckets);
+  const int per = causal != 0 ? n_buckets : n_buckets / 2, alone = std::max(1, per / 2);
+  if (max_distance <= alone)
+    return fail(DSATTN_EINVAL, "max_distance must be > %d (got %d)", alone, max_distance);
+  if (bucket_out == nullptr) return fail(DSATTN_EINVAL, "bucket_out must be non-null");
+  if (!host_writable(bucket_out)) return fail(DSATTN_EINVAL, "bucket_out must be host memory");
+  // The bucket of distance a by its definition, with room for the rounding of the logarithms
+  // where a lies on a border (an exact ratio of powers).
+  const long double scale = (long double)(per - alone) / std::log((long double)max_distance / alone);
+  auto f = [&](int a) {
+    if (a < alone) return a;
+    if (a >= max_distance) return per - 1;
+    const long double x = std::log((long double)a / alone) * scale;
+    return std::min(per - 1, alone + (int)std::floor(x + 1e-15L * (1 + x)));
+  };
+  // f is monotonous: walk the distances away from zero and evaluate it only while it changes
+  const int back_most = q_first + n_q - 1;              // -d of the first key and the last query
+  const int fore_most = n_k - 1 - q_first;              // d of the last key and the first query
+  auto fill = [&](int a, int32_t b) {                   // distance -a (a < 0: the key comes later)
+    const long long e = (long long)back_most - a;
+    if (e >= 0 && e < (long long)n_q + n_k - 1) bucket_out[e] = b;
+  };
+  for (int a = 0, b = 0; a <= back_most; ++a) {
+    if (b < per - 1) b = f(a);
+    fill(a, b);
+  }
+  for (int a = 1, b = 0; a <= fore_most; ++a) {
+    if (b < per - 1) b = f(a);
+    fill(-a, causal != 0 ? -1 : per + b);
+  }
   g_last_error.clear();
   return DSATTN_OK;
 }

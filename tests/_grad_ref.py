@@ -2,8 +2,8 @@
 elementwise bounds of what a kernel with bf16 operands and 32-bit sums may be off by.
 
 Half a step of a rounding is U16 = 2^-8 (bf16) or U32 = 2^-24 of the value.  The kernels round
-P and dS to bf16 for the products, and the results to bf16; they take delta from the bf16
-output of the forward pass.  Per logit the 32-bit arithmetic is off by at most ETA (128 products
+P and dS to bf16 for the products, and the results to bf16.  They sum delta in 32 bits; only dq
+begins with the rounded output's delta' and corrects for it afterwards.  Per logit the 32-bit arithmetic is off by at most ETA (128 products
 and their sum, the product with the scale, the difference to the LSE and the LSE's own
 rounding), and exp2 and log2 by a few units in the last place.
 """
@@ -18,16 +18,19 @@ U16, U32 = 2.0 ** -8, 2.0 ** -24
 class Ref:
     """o, lse, dq, dk, dv, ds (float64) and bounds b_o, b_lse, b_dq, b_dk, b_dv of one problem
     q [B, H, n_q, d], k, v [B, H, n_k, d], do like q (or None).  bias [H or 1, n_q, n_k] in
-    natural units (-inf: closed); skip [B, H, n_q, n_k] bool."""
+    natural units (-inf: closed); skip [B, H, n_q, n_k] bool.  library_forward: the kernel gets o
+    and the LSE from a forward call, which is off by their own bounds, not rounded from here."""
 
-    def __init__(self, q, k, v, do=None, scale=None, bias=None, skip=None):
+    def __init__(self, q, k, v, do=None, scale=None, bias=None, skip=None, library_forward=False):
         q, k, v = (x.detach().double() for x in (q, k, v))
         scale = 1.0 / math.sqrt(q.shape[-1]) if scale is None else scale
         t = lambda x: x.transpose(-1, -2).contiguous()
         s = scale * (q @ t(k))
         size = scale * (q.abs() @ t(k.abs()))
         if bias is not None:
-            s = s + bias.double()
+            bias = bias.double()
+            s = s + bias
+            size = size + bias.masked_fill(torch.isinf(bias), 0.0).abs()
         if skip is not None:
             s = s.masked_fill(skip, -math.inf)
         lse = torch.logsumexp(s, -1)
@@ -52,15 +55,32 @@ class Ref:
         self.dv = t(self.p) @ do
         self.dq = scale * (self.ds @ k)
         self.dk = scale * (t(self.ds) @ q)
-        # delta: the rounded output, 128 products in 32 bits
-        d_delta = ((U16 + 130 * U32) * self.o.abs() * do.abs()).sum(-1, keepdim=True)
+        if library_forward:
+            rel = rel + 2 * self.b_lse[..., None]
+        d_o = self.b_o if library_forward else U16 * self.o.abs()
         d_dp = 130 * U32 * (do.abs() @ t(v.abs()))
-        self.b_ds32 = rel * self.ds.abs() + self.p * (d_dp + d_delta + 2 * U32 * (dp.abs() + delta.abs()))
-        b_ds = U16 * self.ds.abs() + 1.01 * self.b_ds32
         n = U32 * max(s.shape[-1], s.shape[-2])
+        # delta as the sum of P dP, and what delta' is off by
+        d_delta = (self.p * (d_dp + (rel + n) * dp.abs())).sum(-1, keepdim=True)
+        d_prime = ((d_o + 130 * U32 * self.o.abs()) * do.abs()).sum(-1, keepdim=True)
+        self.b_ds = 1.01 * (rel * self.ds.abs() + self.p * (d_dp + d_delta + 2 * U32 * (dp.abs() + delta.abs())))
+        b_k = self.b_ds + (U16 + n) * self.ds.abs()
+        # dq: the rounding of P (dP - delta') and of P in the correction
+        b_q = b_k + 2 * (U16 + n + rel) * self.p * (d_prime + d_delta)
         self.b_dv = U16 * self.dv.abs() + t((U16 + n + rel) * self.p) @ do.abs()
-        self.b_dq = U16 * self.dq.abs() + scale * ((b_ds + n * self.ds.abs()) @ k.abs())
-        self.b_dk = U16 * self.dk.abs() + scale * (t(b_ds + n * self.ds.abs()) @ q.abs())
+        self.b_dq = U16 * self.dq.abs() + scale * (b_q @ k.abs())
+        self.b_dk = U16 * self.dk.abs() + scale * (t(b_k) @ q.abs())
+
+    def add_table(self, bucket, n_buckets):
+        """dtable [n_buckets, H] and b_dtable; bucket [n_q, n_k] of every pair, -1: closed."""
+        at = bucket.flatten().clamp(min=0).long()
+        closed = (bucket < 0).flatten()
+        for name, x in (("dtable", self.ds),
+                        ("b_dtable", self.b_ds + U32 * bucket.numel() ** 0.5 * self.ds.abs())):
+            x = x.sum(0).flatten(1).masked_fill(closed, 0.0)
+            out = torch.zeros(x.shape[0], n_buckets, dtype=torch.float64, device=x.device)
+            setattr(self, name, out.index_add_(1, at, x).t().contiguous())
+        self.b_dtable = self.b_dtable + 2 * U32 * self.dtable.abs()
 
     def check(self, **got):
         """Every named result within its bound, elementwise; returns the largest share used."""
@@ -78,6 +98,12 @@ class Ref:
             worst[name] = use
             assert use <= 1.0, f"{name}: {use:.2f} of its bound"
         return worst
+
+
+def distance_matrix(x, n_q, n_k):
+    """[..., n_q, n_k] of x [..., n_q + n_k - 1] over key - query, from -(n_q - 1) up."""
+    i = torch.arange(n_q, device=x.device)[:, None]
+    return x[..., torch.arange(n_k, device=x.device)[None, :] - i + n_q - 1]
 
 
 def skip_pairs(mask, N, tile_q, tile_k):

@@ -30,7 +30,9 @@ def header_fields(struct):
     return names
 
 
-@pytest.mark.parametrize("struct,mirror", [("dsattn_bwd_args", "DsAttnBwdArgs")])
+@pytest.mark.parametrize("struct,mirror", [("dsattn_bwd_args", "DsAttnBwdArgs"),
+                                           ("dsattn_bias_args", "DsAttnBiasArgs"),
+                                           ("dsattn_bias_bwd_args", "DsAttnBiasBwdArgs")])
 def test_struct_mirrors(struct, mirror):
     pkg = _lib()
     assert header_fields(struct) == [f[0] for f in getattr(pkg, mirror)._fields_]
@@ -95,6 +97,105 @@ def test_workspace_sizes():
     assert size(1, 1, 1) == 2 * 256 and size(1, 1, 65) == 2 * 512
     assert size(2, 40, 32760) == 2 * 80 * 32768 * 4
     assert size(70000, 1, 1) == 0 and size(1, 1, 1 << 24) == 0
+
+
+def bias_call(pkg, backward, **kw):
+    x = dict(B=1, H=2, n_q=64, n_k=64, d=128, n_buckets=8, scale=0.1)
+    if not backward:
+        x["k_rows"] = kw.get("n_k", 64)
+    x.update(kw)
+    L = pkg.lib()
+    if backward:
+        return L.dsattn_bias_attn_bwd(ctypes.byref(pkg.DsAttnBiasBwdArgs(**x)), None, 0)
+    return L.dsattn_bias_attn_fwd(ctypes.byref(pkg.DsAttnBiasArgs(**x)), None, 0)
+
+
+@pytest.mark.parametrize("backward", [False, True])
+@pytest.mark.parametrize("kw,rc,message", [
+    (dict(B=-1), -1, ">= 0"),
+    (dict(n_q=-1), -1, ">= 0"),
+    (dict(n_k=-1), -1, ">= 0"),
+    (dict(scale=float("inf")), -1, "scale"),
+    (dict(d=256), -2, "head dimension"),
+    (dict(n_buckets=0), -2, "n_buckets"),
+    (dict(n_buckets=513), -2, "n_buckets"),
+    (dict(B=65536), -1, "65535"),
+    (dict(n_q=8388608), -1, "8388607"),
+    (dict(n_k=8388608), -1, "8388607"),
+    (dict(B=1000, H=60, n_q=8388607), -1, "too large"),
+    (dict(), -1, "workspace must be non-null"),
+])
+def test_bias_refusals(backward, kw, rc, message):
+    pkg = _lib()
+    assert bias_call(pkg, backward, **kw) == rc
+    assert message in pkg.last_error()
+
+
+def test_bias_cache_and_empty_problems():
+    pkg = _lib()
+    assert bias_call(pkg, False, n_k=64, k_rows=63) == -1
+    assert "k_rows must be >= n_k" in pkg.last_error()
+    for kw in (dict(B=0), dict(H=0), dict(n_q=0)):
+        assert bias_call(pkg, False, **kw) == 0
+    assert bias_call(pkg, True, H=0) == 0
+    assert pkg.lib().dsattn_bias_attn_fwd(None, None, 0) == -1
+    assert pkg.lib().dsattn_bias_attn_bwd(None, None, 0) == -1
+
+
+def test_bias_workspace_sizes():
+    pkg = _lib()
+    fwd, bwd = pkg.dsattn_bias_attn_workspace_bytes, pkg.dsattn_bias_attn_bwd_workspace_bytes
+    assert fwd(0, 2, 5, 5) == fwd(1, 0, 5, 5) == fwd(1, 2, 0, 5) == fwd(-1, 2, 5, 5) == 0
+    assert bwd(1, 0, 5, 5, 8) == bwd(1, 2, 5, 5, 0) == bwd(1, 2, 5, 5, 513) == 0
+    assert fwd(1, 2, 5, 0) > 0 and bwd(0, 2, 5, 5, 8) > 0
+    # few queries: the splits' parts come on top of the layout by distance
+    one = fwd(1, 40, 1, 32760)
+    assert one > 40 * 32760 * 4 and one < 40 * 32760 * 4 + (64 << 20)
+    for shape in ((1, 40, 1, 32760), (2, 3, 100, 5000), (1, 1, 1, 1), (1, 2, 8000000, 3)):
+        assert fwd(*shape) % 256 == 0 and bwd(*shape, 32) % 256 == 0
+
+
+def buckets_by_definition(n_q, n_k, q_first, n_buckets, max_distance, causal):
+    """In whole numbers: far distance a has bucket E + k where (a / E)^(P - E) lies between the
+    k-th and the next power of max_distance / E."""
+    P = n_buckets if causal else n_buckets // 2
+    E = max(1, P // 2)
+
+    def f(a):
+        if a < E:
+            return a
+        k = 0
+        while k < P - E and a ** (P - E) * E ** (k + 1) >= max_distance ** (k + 1) * E ** (P - E):
+            k += 1
+        return min(P - 1, E + k)
+
+    out = []
+    for e in range(n_q + n_k - 1):
+        d = e - (n_q - 1) - q_first
+        out.append(f(-d) if d <= 0 else -1 if causal else P + f(d))
+    return out
+
+
+@pytest.mark.parametrize("n_q,n_k,q_first,n_buckets,max_distance,causal", [
+    (1, 1, 0, 2, 8, False), (5, 7, 0, 32, 128, False), (400, 300, 0, 32, 128, False),
+    (400, 300, 17, 32, 128, True), (1, 700, 699, 16, 512, True), (3, 40, 500, 9, 60, False),
+    (300, 300, 0, 121, 60, False), (300, 300, 0, 3, 5, True), (130, 130, 0, 64, 1024, False)])
+def test_relative_buckets(n_q, n_k, q_first, n_buckets, max_distance, causal):
+    pkg = _lib()
+    got = pkg.dsattn_relative_buckets(n_q, n_k, n_buckets, max_distance, q_first=q_first,
+                                      causal=causal)
+    assert got.tolist() == buckets_by_definition(n_q, n_k, q_first, n_buckets, max_distance, causal)
+
+
+@pytest.mark.parametrize("args", [(0, 1, 32, 128), (1, 0, 32, 128), (8388608, 1, 32, 128),
+                                  (1, 1, 1, 128), (1, 1, 32, 8), (1, 1, 32, -5)])
+def test_relative_buckets_refusals(args):
+    pkg = _lib()
+    with pytest.raises(RuntimeError):
+        pkg.dsattn_relative_buckets(*args)
+    with pytest.raises(RuntimeError):
+        pkg.dsattn_relative_buckets(4, 4, 32, 128, q_first=-1)
+    assert pkg.lib().dsattn_relative_buckets(4, 4, 0, 32, 128, 0, None) == -1
 
 
 @pytest.mark.parametrize("bias,skip", [(False, False), (True, False), (False, True), (True, True)])
