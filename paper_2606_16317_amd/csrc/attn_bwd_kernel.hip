@@ -4,20 +4,21 @@
 //   dV = P^T dO      dK = scale dS^T Q    dQ = scale dS K
 //
 // Two kernels share the work: one owns keys and streams queries (dK, dV: four products), one
-// owns queries and streams keys (dQ: three products).  One kernel for all would need five
-// products instead of seven, but would have to add every workgroup's part of dQ in memory:
-// 64 KiB of fp32 atomics for each 21 MFLOP, in an order that changes from run to run.  Seven
-// products at the rate of the forward pass cost less than five with those, and their sums are
-// always in the same order.
+// owns queries and streams keys (dQ: three products, and a fourth for its accuracy, see there).
+// One kernel for all would need five products instead of eight, but would have to add every
+// workgroup's part of dQ in memory: 64 KiB of fp32 atomics for each 21 MFLOP, in an order that
+// changes from run to run.  Two kernels' sums are always in the same order.
 //
 // Both are bound by MFMA and, equally, by LDS reads (1 KiB of operand per MFMA, the other
 // operand stays in registers).  Instruction order is fixed by fences: operands are read two
 // MFMAs ahead, exponentials run under the dP products, dS under the dV products.
-// N = 32760, 10 heads: 16.1 ms, 852 TFLOP/s of the five products the mathematics needs and
-// 1193 of the seven computed; a large library product reaches 1215 on the same card.
+// N = 32760, 10 heads: 18.8 ms, 730 TFLOP/s of the five products the mathematics needs and
+// 1170 of the eight computed; a large library product reaches 1215 on the same card.
 
 #include "attn_bwd_launch.h"
 #include "attn_tiles.h"
+
+#include <type_traits>
 
 namespace dsattn {
 namespace {
@@ -135,13 +136,80 @@ __device__ __forceinline__ void open_tiles(TileRange& range, const BiasParams& b
   __syncthreads();
 }
 
-// The run that a 32 x 32 block lies in (its 63 distances begin at word m of the runs of its
-// tile), or kRunMixed.
-__device__ __forceinline__ int block_run(const int32_t (&runs)[64], int m) {
-  const int x = __builtin_amdgcn_readfirstlane(runs[m]);
-  const int y = __builtin_amdgcn_readfirstlane(runs[m + 1]);
-  const int z = __builtin_amdgcn_readfirstlane(runs[m + 2]);
-  return x == y && y == z ? x : (int)kRunMixed;
+// What a wave's two 32 x 32 blocks of a tile lie in, by ascending distance: run[j] as a word of
+// runs, but with the position counted from the tile's smallest distance, and the value at the
+// block's first query and key.  A block's 63 distances begin in word m (m + 1 for the second) of
+// the tile's words and end at most two words on; what lies in them beyond the block may make it
+// count as less even than it is, which costs time only.  start: distance index of word 0 (at or
+// below the tile's smallest); flat[b] is read from value[step b].
+struct TileRuns {
+  int run[2];
+  float flat[2];
+  __device__ __forceinline__ void read(const int32_t (&runs)[64], int m, int start, const float* value,
+                                       int step) {
+    int x[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) x[j] = __builtin_amdgcn_readfirstlane(runs[m + j]);
+    const float f = value[0];
+    flat[0] = flat[1] =
+        __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, f)));
+    run[0] = run[1] = x[0];
+    if (x[0] == x[1] && x[0] == x[2] && x[0] == x[3] && !is_step(x[0])) return;   // nearly always
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      int steps = 0, cut = 0;
+#pragma unroll
+      for (int i = 0; i < 3; ++i) {
+        const int y = x[j + i], at = 32 * (m + j + i) + start;
+        if (y == kRunMixed) steps = 2;
+        if (is_step(y)) {
+          steps += 1;
+          cut = at + run_pos(y);
+        }
+        if (i < 2 && run_last(y) != run_first(x[j + i + 1])) {
+          steps += 1;
+          cut = at + 32;
+        }
+      }
+      run[j] = steps == 0   ? x[j]
+               : steps == 1 ? run_step(run_first(x[j]), run_last(x[j + 2]), max(cut, 0))
+                            : (int)kRunMixed;
+      flat[j] = __builtin_bit_cast(
+          float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, value[step * j])));
+    }
+  }
+};
+
+// Whether a run is one bucket (or closed) throughout.
+__device__ __forceinline__ bool is_flat(int run) { return run != kRunMixed && !is_step(run); }
+
+// Sum over a wave, in every lane.  (Data-parallel moves within the vector unit: the shuffles'
+// way through LDS takes ten times as long.)
+__device__ __forceinline__ float wave_sum(float x) {
+  auto add = [&](auto ctrl, auto rows) {
+    x += __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x),
+                                                               decltype(ctrl)::value,
+                                                               decltype(rows)::value, 0xf, false));
+  };
+  add(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});   // row_shr 1
+  add(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
+  add(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});   // row_bcast 15
+  add(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});   // row_bcast 31
+  return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
+}
+
+// Head and 128-row group of a workgroup.  A bias that closes later keys leaves the first key group
+// and the last query group the most to do: with a bias these come first for all heads, so that no
+// long one starts late.  (Otherwise a head's groups stand together, whose tiles L2 then shares.)
+template <int MODE>
+__device__ __forceinline__ int group_head(const BwdParams& p) {
+  return MODE == kBwdBias ? (int)(blockIdx.x % (unsigned)p.bh) : (int)blockIdx.y;
+}
+template <int MODE>
+__device__ __forceinline__ int group_index(const BwdParams& p) {
+  return MODE == kBwdBias ? (int)(blockIdx.x / (unsigned)p.bh) : (int)blockIdx.x;
 }
 
 // ---- dk, dv ------------------------------------------------------------------------------
@@ -184,12 +252,13 @@ struct DkvSmem {
   typename SideOf<MODE, DkvBias>::type side;
 };
 
-// The bias of a 32 x 32 block: the run it lies in, its value there, and where this lane reads
-// the single values of a mixed block.
+// The bias of a 32 x 32 block: the run it lies in, its value there, and where the single values
+// of a mixed block begin.
 struct BlockBias {
   int run;
   float flat;
-  const float* win;
+  const float* win;   // of the block's smallest distance
+  int first;          // the same, counted from the tile's
 };
 
 __device__ __forceinline__ void lds_add(float* p, float x) {
@@ -203,24 +272,24 @@ __device__ __forceinline__ constexpr int back(int v) { return 27 - 8 * (v >> 2) 
 // queries: S = Q K^T and dP = dO V^T with keys as columns, so that
 // P and dS are B operands of dV^T += dO^T P and dK^T += Q^T dS.
 template <int MODE>
-__device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int b, uint32_t row_at,
+__device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uint32_t row_at,
                                           uint32_t col_at, const bf16x8 (&kf)[8],
                                           const bf16x8 (&vf)[8], f32x16 (&dk)[4],
-                                          f32x16 (&dv)[4], float c, int g, const BlockBias& bias, float& far) {
-  constexpr int kG = 2 * kTileElems * 2;   // bytes from the q tiles to the dO tiles
+                                          f32x16 (&dv)[4], float c, int lane, int w, bool there,
+                                          const BlockBias& bias, float& all, float& below) {
+  const uint32_t q_at = lds_addr(sm.q), g_at = lds_addr(sm.g);
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
-  row_at += block;
-  col_at += block;
-  here(row_at);
-  here(col_at);
+  const int g = lane >> 5;
   f32x16 s = f32x16{}, dp, nd;
   if constexpr (MODE == kBwdBias) {
-    if (bias.run == kRunMixed) {
+    if (!is_flat(bias.run)) {
+      const float* win = there ? bias.win + 4 + (lane & 31) - 4 * g : sm.side.closed;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = bias.win[back(v)];
+      for (int v = 0; v < 16; ++v) s[v] = win[back(v)];
     } else {
+      const float flat = there ? bias.flat : neg_inf();
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = bias.flat;
+      for (int v = 0; v < 16; ++v) s[v] = flat;
     }
   }
   float sum = 0.f;
@@ -237,8 +306,8 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
   };
   // A operands in the order of their products: S, dP, dV, dK (eight each)
   auto operand = [&](int i) {
-    if (i < 16) return row_operand(row_at, i < 8 ? 0 : kG, i & 7);
-    return col_operand(col_at, i < 24 ? kG : 0, (i & 7) >> 2, i & 3);
+    if (i < 16) return row_operand(row_at, block, i < 8 ? q_at : g_at, i & 7);
+    return col_operand(col_at, block, i < 24 ? g_at : q_at, (i & 7) >> 2, i & 3);
   };
   bf16x8 pf[2], df[2];
   auto prob = [&](int v) {
@@ -248,7 +317,10 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
   auto grad = [&](int v) {
     const float x = s[v] * dp[v];
     df[v >> 3][v & 7] = (__bf16)x;
-    if constexpr (MODE == kBwdBias) sum += x;
+    if constexpr (MODE == kBwdBias) {
+      sum += x;
+      s[v] = x;
+    }
   };
   constexpr int RK = 3;
   bf16x8 a[RK];
@@ -276,60 +348,92 @@ __device__ __forceinline__ void dkv_block(const DkvSmem<MODE>& sm, int buf, int 
       if (i >= 16 && i < 20 && e < 1) prob(i - 4);
       if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
+    // dS in 32 bits, now in s, while it is there: of a mixed block by distance, of one with a
+    // step the part below it; the sum of all of it comes from grad
+    if constexpr (MODE == kBwdBias) {
+      if (i == 23) {
+        below = 0.f;
+        if (is_step(bias.run)) {
+          const int cut = run_pos(bias.run) - bias.first - 4 - (lane & 31) + 4 * g;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) below += back(v) < cut ? s[v] : 0.f;
+        } else if (bias.run == kRunMixed) {
+          float* diag = &sm.side.diag[w][g][(lane & 31) + 4 - 4 * g];
+#pragma unroll
+          for (int v = 0; v < 16; ++v) lds_add(diag + back(v), s[v]);
+        }
+      }
+    }
     sched_fence();
   }
-  // dS in 32 bits, where all of the block is one bucket's
-  if constexpr (MODE == kBwdBias) far += bias.run == kRunMixed ? 0.f : sum;
+  all = sum;
 }
 
-// dS of a mixed block by distance, in 32 bits: S and dP once more.  (Within dkv_block the 16
-// values would have to outlive the dV products, for which there are no registers; few blocks are
-// mixed.)
-__device__ __forceinline__ void diag_block(const DkvSmem<kBwdBias>& sm, int buf, int b,
-                                           uint32_t row_at, const bf16x8 (&kf)[8],
-                                           const bf16x8 (&vf)[8], float c, int g,
-                                           const float* win, float* diag) {
-  constexpr int kG = 2 * kTileElems * 2;
-  row_at += (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
-  here(row_at);
-  f32x16 s, dp;
-#pragma unroll
-  for (int v = 0; v < 16; ++v) {
-    s[v] = win[back(v)];
-    dp[v] = sm.nd[buf][32 * b + 4 * g + 27 - back(v)];
+// Sums over block elements that are not in the bins yet: of two buckets, since blocks come by
+// descending distance and one with a step is followed by others with the same, until one lies
+// below it.  A lane's part is a sum of block sums of 16, the bins take sums of at most 64 blocks:
+// errors grow with the root of each count.
+struct FarSums {
+  int run = kRunClosed, next = kRunClosed;
+  float x = 0.f, y = 0.f;   // of run and of next
+  __device__ __forceinline__ static void put(float* bins, int run, float x, int lane) {
+    const float total = wave_sum(x);
+    if (lane == 0 && run >= 0) lds_add(&bins[run], total);
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    s = mfma(row_operand(row_at, 0, i), kf[i], s);
-    dp = mfma(row_operand(row_at, kG, i), vf[i], dp);
-    sched_fence();
+  __device__ __forceinline__ void flush(float* bins, int lane) {
+    put(bins, run, x, lane);
+    put(bins, next, y, lane);
+    run = next = kRunClosed;
+    x = y = 0.f;
   }
-#pragma unroll
-  for (int v = 0; v < 16; ++v)
-    lds_add(diag + back(v),
-            exp2_fast(fmaf(s[v], c, sm.nl[buf][32 * b + 4 * g + 27 - back(v)])) * dp[v]);
-}
-
-// Add the sum over one run's elements to its bucket.  (A lane's far is a sum of block sums of 16,
-// the bins take sums of at most 64 blocks: errors grow with the root of each count.)
-__device__ __forceinline__ void flush_far(float* bins, int run, float& far, int lane) {
-  float x = far;
-#pragma unroll
-  for (int m = 32; m >= 1; m >>= 1) x += __shfl_xor(x, m);
-  if (lane == 0 && run >= 0) lds_add(&bins[run], x);
-  far = 0.f;
-}
+  // One block's sums: `all` of it, and what lies below its step.
+  __device__ __forceinline__ void add(float* bins, int block, float all, float below, int lane) {
+    if (block == run) {   // nearly always
+      x += all;
+      return;
+    }
+    const int high = run_last(block), low = run_first(block);
+    if (high == next) {   // the step lies behind
+      put(bins, run, x, lane);
+      run = next;
+      x = y;
+      next = kRunClosed;
+      y = 0.f;
+    }
+    if (high != run || (low != high && next != kRunClosed && next != low)) {
+      flush(bins, lane);
+      run = high;
+    }
+    x += all - below;
+    if (low != high) {
+      next = low;
+      y += below;
+    }
+  }
+};
 
 // Add a mixed block's sums by distance to their buckets, and clear them.  All of it is one
-// wave's: its LDS accesses run in order.
+// wave's: its LDS accesses run in order.  A bucket that many of the distances share is summed up
+// first: atomics on one address wait for each other.
 __device__ __forceinline__ void flush_diag(float (&diag)[2][64], const int32_t* bucket, float* bins,
                                            int n_buckets, int lane) {
   asm volatile("" ::: "memory");
   const float x = diag[0][lane] + diag[1][lane];
-  const int at = bucket[lane];
+  int at = bucket[lane];
   diag[0][lane] = 0.f;
   diag[1][lane] = 0.f;
-  if (lane < 63 && (uint32_t)at < (uint32_t)n_buckets) lds_add(&bins[at], x);
+  if (lane == 63 || (uint32_t)at >= (uint32_t)n_buckets) at = kRunClosed;
+  // the ends of the range are where wide buckets are
+#pragma unroll
+  for (int end = 0; end < 2; ++end) {
+    const int wide = __builtin_amdgcn_readlane(at, end == 0 ? 0 : 62);
+    if (wide >= 0 && __popcll(__ballot(at == wide)) >= 8) {
+      const float total = wave_sum(at == wide ? x : 0.f);
+      if (lane == 0) lds_add(&bins[wide], total);
+      if (at == wide) at = kRunClosed;
+    }
+  }
+  if (at >= 0) lds_add(&bins[at], x);
   asm volatile("" ::: "memory");
 }
 
@@ -338,15 +442,14 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   __shared__ DkvSmem<MODE> sm;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = blockIdx.y;
-  const int key0 = blockIdx.x * 128;
+  const int bh = group_head<MODE>(p), key0 = group_index<MODE>(p) * 128;
   const int n_tiles = (p.n_q + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto qrs = row_buffer(p.q + qoff, p.n_q), grs = row_buffer(p.dout + qoff, p.n_q);
   const auto lrs = word_buffer(p.neg_lse2 + (size_t)bh * p.n_rows, p.n_rows);
   const auto drs = word_buffer(p.neg_delta + (size_t)bh * p.n_rows, p.n_rows);
   const uint32_t off = tile_lane_offset(w, lane);
-  const uint32_t row_at = lds_addr(sm.q) + row_lane(r, g), col_at = lds_addr(sm.q) + col_lane(lane);
+  const uint32_t row_at = row_lane(r, g), col_at = col_lane(lane);
   const auto first_distance = [&](int t) { return key0 - (t * kTile + 63) + p.n_q - 1; };
   const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
   const auto brs = word_buffer(p.bias.bucket, p.bias.n_dist), rrs = word_buffer(p.bias.runs, p.bias.n_runs);
@@ -398,42 +501,49 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   // compiler moves all accumulators between the loops
   const bool own = key0 + 32 * w < p.n_k;   // this wave has a key
   uint32_t bits = 0xffu;
-  BlockBias bias{};
-  int far_run = kRunClosed;   // the run of the blocks whose sum is in far
-  float far = 0.f;
+  TileRuns tile{};
+  FarSums far;
   for (int i = 0; i < 2 * count; ++i) {
     const int buf = i >> 1 & 1, b = i & 1;
     if (b == 0) {
       tiles_ready();
       if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
       if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
+      if constexpr (MODE == kBwdBias)
+        tile.read(sm.side.runs[buf], w, -(first_distance(tile_at(i >> 1)) & 31),
+                  &sm.side.win[buf][32 * w + 63], -32);
     }
     bool visit = own;
     if constexpr (MODE == kBwdMask) visit = bits >> (4 * b + w) & 1u;
+    BlockBias bias{};
     if constexpr (MODE == kBwdBias) {
-      bias.run = block_run(sm.side.runs[buf], 1 + w - b);
+      bias.run = b == 0 ? tile.run[1] : tile.run[0];
+      bias.flat = b == 0 ? tile.flat[0] : tile.flat[1];
+      bias.first = 32 * w + 32 - 32 * b;
+      bias.win = &sm.side.win[buf][bias.first];
       visit = own && bias.run != kRunClosed;
-      bias.win = key < p.n_k ? &sm.side.win[buf][32 * w + r - 4 * g + 36 - 32 * b] : sm.side.closed;
-      bias.flat = key < p.n_k ? sm.side.win[buf][32 * w - 32 * b + 63] : neg_inf();
-      if (visit && bias.run == kRunMixed) {
-        diag_block(sm, buf, b, row_at, kf, vf, p.c, g, bias.win, &sm.side.diag[w][g][r - 4 * g + 4]);
-        flush_diag(sm.side.diag[w], &sm.side.bucket[buf][32 * w - 32 * b + 32], sm.side.bins[w],
-                   p.bias.n_buckets, lane);
-      } else if (visit && (bias.run != far_run || (i & 63) == 0)) {
-        flush_far(sm.side.bins[w], far_run, far, lane);
-        far_run = bias.run;
-      }
     }
-    if (visit) dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, g, bias, far);
+    float all = 0.f, below = 0.f;
+    if (visit)
+      dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, lane, w, key < p.n_k, bias,
+                      all, below);
+    if constexpr (MODE == kBwdBias) {
+      if (visit && bias.run == kRunMixed)
+        flush_diag(sm.side.diag[w], &sm.side.bucket[buf][bias.first], sm.side.bins[w],
+                   p.bias.n_buckets, lane);
+      else if (visit)
+        far.add(sm.side.bins[w], bias.run, all, below, lane);
+      if ((i & 63) == 63) far.flush(sm.side.bins[w], lane);
+    }
   }
   if (key < p.n_k) {
     store_row(p.dv + koff, key, dv, 1.f, g);
     store_row(p.dk + koff, key, dk, p.scale, g);
   }
   if constexpr (MODE == kBwdBias) {
-    flush_far(sm.side.bins[w], far_run, far, lane);
+    far.flush(sm.side.bins[w], lane);
     __syncthreads();
-    float* part = p.dtable_part + ((size_t)bh * gridDim.x + blockIdx.x) * p.bias.n_buckets;
+    float* part = p.dtable_part + ((size_t)bh * ((p.n_k + 127) / 128) + key0 / 128) * p.bias.n_buckets;
     for (int i = tid; i < p.bias.n_buckets; i += kThreads)
       part[i] = (sm.side.bins[0][i] + sm.side.bins[1][i]) + (sm.side.bins[2][i] + sm.side.bins[3][i]);
   }
@@ -457,23 +567,20 @@ struct DqSmem {
 // dQ = scale (sum of P (dP - delta') k - (delta - delta') sum of P k), and the dk, dv kernel gets
 // delta.  The fourth product, sum of P k, is its price: without it, dq and dk were off by 4.5e-3
 // of their norm at N = 32760 instead of 2e-3.
-template <int MODE>
-__device__ __forceinline__ void dq_block(int buf, int b, uint32_t row_at, uint32_t col_at,
+template <int MODE, bool TAIL>
+__device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint32_t row_at, uint32_t col_at,
                                          const bf16x8 (&qf)[8], const bf16x8 (&gf)[8],
                                          f32x16 (&dq)[4], f32x16 (&pk)[4], float nl, float nd,
-                                         float c, int g, int left,
+                                         float c, int lane, int left,
                                          int run, float flat, const float* win, float& delta, float& rest) {
-  constexpr int kV = 2 * kTileElems * 2;   // bytes from the k tiles to the v tiles
+  const uint32_t k_at = lds_addr(sm.k), v_at = lds_addr(sm.v);
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
-  row_at += block;
-  col_at += block;
-  here(row_at);
-  here(col_at);
   f32x16 s = f32x16{}, dp;
   if constexpr (MODE == kBwdBias) {
-    if (run == kRunMixed) {
+    if (!is_flat(run)) {
+      const float* at = win + 4 * (lane >> 5) - (lane & 31);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = win[27 - back(v)];
+      for (int v = 0; v < 16; ++v) s[v] = at[27 - back(v)];
     } else {
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = flat;
@@ -483,8 +590,8 @@ __device__ __forceinline__ void dq_block(int buf, int b, uint32_t row_at, uint32
   bf16x8 pf[2], df[2];
   // A operands in the order of their products: S, dP, P K, dQ (eight each)
   auto operand = [&](int i) {
-    if (i < 16) return row_operand(row_at, i < 8 ? 0 : kV, i & 7);
-    return col_operand(col_at, 0, (i & 7) >> 2, i & 3);
+    if (i < 16) return row_operand(row_at, block, i < 8 ? k_at : v_at, i & 7);
+    return col_operand(col_at, block, k_at, (i & 7) >> 2, i & 3);
   };
   auto prob = [&](int v) {
     s[v] = exp2_fast(fmaf(s[v], c, nl));
@@ -512,10 +619,10 @@ __device__ __forceinline__ void dq_block(int buf, int b, uint32_t row_at, uint32
     else
       dq[i & 3] = mfma(x, df[(i & 7) >> 2], dq[i & 3]);
     // keys past the end: their rows are zeros, but exp2(-lse) may be infinite
-    if (i == 8 && left < 32) {
+    if (TAIL && i == 8) {
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        if (27 - back(v) + 4 * g >= left) s[v] = neg_inf();
+        if (27 - back(v) + 4 * (lane >> 5) >= left) s[v] = neg_inf();
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {   // as in dkv_block
@@ -536,14 +643,14 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   __shared__ DqSmem<MODE> sm;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = blockIdx.y;
-  // with a bias that closes later keys, the last queries have the most to do: they go first
-  const int q0 = (MODE == kBwdBias ? (int)(gridDim.x - 1 - blockIdx.x) : (int)blockIdx.x) * 128;
+  const int bh = group_head<MODE>(p);
+  const int group = group_index<MODE>(p), n_groups = (p.n_q + 127) / 128;
+  const int q0 = (MODE == kBwdBias ? n_groups - 1 - group : group) * 128;
   const int n_tiles = (p.n_k + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
   const uint32_t off = tile_lane_offset(w, lane);
-  const uint32_t row_at = lds_addr(sm.k) + row_lane(r, g), col_at = lds_addr(sm.k) + col_lane(lane);
+  const uint32_t row_at = row_lane(r, g), col_at = col_lane(lane);
   const auto first_distance = [&](int t) { return t * kTile - (q0 + 127) + p.n_q - 1; };
   const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
   const auto rrs = word_buffer(p.bias.runs, p.bias.n_runs);
@@ -578,36 +685,47 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const int row = q0 + w * 32 + r;
   load_row(qf, p.q + qoff, row, row < p.n_q, g);
   load_row(gf, p.dout + qoff, row, row < p.n_q, g);
-  const size_t at = (size_t)bh * p.n_rows + row;
-  const float nl = row < p.n_q ? p.neg_lse2[at] : neg_inf();
-  const float nd = row < p.n_q ? p.neg_delta[at] : 0.f;
+  float nl = neg_inf(), nd = 0.f;
+  if (row < p.n_q) {
+    nl = p.neg_lse2[(size_t)bh * p.n_rows + row];
+    nd = p.neg_delta[(size_t)bh * p.n_rows + row];
+  }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
   const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
   uint32_t bits = 0xffu;
-  int t = 0, run = kRunMixed;
-  float delta = 0.f, rest = 0.f, flat = 0.f;
-  const float* win = nullptr;
-  for (int i = 0; i < 2 * count; ++i) {
-    const int buf = i >> 1 & 1, b = i & 1;
-    if (b == 0) {
-      t = tile_at(i >> 1);
-      tiles_ready();
-      if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
-      if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
+  TileRuns tile{};
+  float delta = 0.f, rest = 0.f;
+  // Visits i0 .. i1 of the 32-key halves.  A ragged last tile has a copy of the block to itself:
+  // masking its keys under a branch in every block took 12 registers, and spilled.
+  auto visit_blocks = [&](auto tail, int i0, int i1) {
+    for (int i = i0; i < i1; ++i) {
+      const int buf = i >> 1 & 1, b = i & 1;
+      if (b == 0) {
+        tiles_ready();
+        if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
+        if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
+        if constexpr (MODE == kBwdBias)
+          tile.read(sm.side.runs[buf], 3 - w, 0, &sm.side.win[buf][127 - 32 * w], 32);
+      }
+      bool visit = own;
+      const float* win = nullptr;
+      if constexpr (MODE == kBwdMask) visit = bits >> (4 * b + w) & 1u;
+      const int run = b == 0 ? tile.run[0] : tile.run[1];
+      if constexpr (MODE == kBwdBias) {
+        visit = own && run != kRunClosed;
+        win = &sm.side.win[buf][32 * b - 32 * w + 127];
+      }
+      if (visit)
+        dq_block<MODE, decltype(tail)::value>(sm, buf, b, row_at, col_at, qf, gf, dq, pk, nl, nd, p.c,
+                                              lane, p.n_k - (n_tiles - 1) * kTile - 32 * b,
+                                              run, b == 0 ? tile.flat[0] : tile.flat[1], win, delta,
+                                              rest);
     }
-    bool visit = own;
-    if constexpr (MODE == kBwdMask) visit = bits >> (4 * b + w) & 1u;
-    if constexpr (MODE == kBwdBias) {
-      run = block_run(sm.side.runs[buf], 3 + b - w);
-      visit = own && run != kRunClosed;
-      flat = sm.side.win[buf][32 * b - 32 * w + 127];
-      win = &sm.side.win[buf][32 * b + 4 * g - 32 * w - r + 127];
-    }
-    if (visit)
-      dq_block<MODE>(buf, b, row_at, col_at, qf, gf, dq, pk, nl, nd, p.c,
-                     g, p.n_k - t * kTile - 32 * b, run, flat, win, delta, rest);
-  }
+  };
+  const bool ragged = count > 0 && p.n_k % kTile != 0 && tile_at(count - 1) == n_tiles - 1;
+  visit_blocks(std::false_type{}, 0, ragged ? 2 * count - 2 : 2 * count);
+  if (ragged) visit_blocks(std::true_type{}, 2 * count - 2, 2 * count);
   const float exact = half_sum(delta + rest), off_by = exact + nd;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
@@ -615,7 +733,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-off_by, pk[db][v], dq[db][v]);
   if (row < p.n_q) {
     store_row(p.dq + qoff, row, dq, p.scale, g);
-    if (g == 0) p.neg_delta[at] = -exact;
+    if (g == 0) p.neg_delta[(size_t)bh * p.n_rows + row] = -exact;
   }
 }
 
@@ -632,10 +750,14 @@ __global__ __launch_bounds__(256) void bias_prepare_kernel(BiasParams b, int H, 
     b.by_dist[(size_t)h * b.dist_stride + e] = x < -1e30f ? neg_inf() : x / scale;
   }
   if (h == 0) {
-    const int first = __shfl(at, threadIdx.x & 32);
-    const uint64_t other = __ballot(there && at != first);
-    if ((threadIdx.x & 31) == 0 && there)
-      b.runs[e >> 5] = (uint32_t)(other >> (threadIdx.x & 32)) == 0 ? at : (int)kRunMixed;
+    // the runs of this half wave: where neighbours differ
+    const int lane = threadIdx.x & 63, half = lane & 32;
+    const int before = __shfl_up(at, 1);
+    const uint32_t change = (uint32_t)(__ballot(there && (lane & 31) != 0 && at != before) >> half);
+    const int pos = __popc(change) == 1 ? __ffs(change) - 1 : 0;
+    const int last = __shfl(at, half + pos);
+    if ((lane & 31) == 0 && there)
+      b.runs[e >> 5] = change == 0 ? at : pos != 0 ? run_step(at, last, pos) : (int)kRunMixed;
   }
 }
 
@@ -659,19 +781,20 @@ __global__ __launch_bounds__(1024) void bias_dtable_kernel(BwdParams p, int B, i
 
 // (Without queries, keys or batches, which only a bias call passes on, the rest still runs.)
 template <int MODE>
-hipError_t launch_mode(const BwdParams& p, int bh, hipStream_t stream) {
+hipError_t launch_mode(const BwdParams& p, hipStream_t stream) {
+  const int bh = p.bh;
+  auto grid = [&](int n) { return MODE == kBwdBias ? dim3((unsigned)n * bh) : dim3(n, bh); };
   if (MODE == kBwdBias) {
     const hipError_t e = launch_bias_prepare(p.bias, p.H, p.scale, stream);
     if (e != hipSuccess) return e;
   }
   if (bh > 0 && p.n_q > 0) {
     hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, bh), dim3(256), 0, stream, p);
-    hipLaunchKernelGGL((bwd_dq_kernel<MODE>), dim3((p.n_q + 127) / 128, bh), dim3(kThreads), 0,
-                       stream, p);
+    hipLaunchKernelGGL((bwd_dq_kernel<MODE>), grid((p.n_q + 127) / 128), dim3(kThreads), 0, stream, p);
   }
   const int groups = bwd_key_groups(p.n_k);
   if (bh > 0 && groups > 0)
-    hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), dim3(groups, bh), dim3(kThreads), 0, stream, p);
+    hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), grid(groups), dim3(kThreads), 0, stream, p);
   if (MODE == kBwdBias)
     hipLaunchKernelGGL(bias_dtable_kernel, dim3((p.bias.n_buckets + 63) / 64, p.H), dim3(1024), 0,
                        stream, p, bh / p.H, groups);
@@ -690,11 +813,11 @@ hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStrea
   return hipGetLastError();
 }
 
-hipError_t launch_attn_bwd(int mode, const BwdParams& p, int bh, hipStream_t stream) {
+hipError_t launch_attn_bwd(int mode, const BwdParams& p, hipStream_t stream) {
   switch (mode) {
-    case kBwdDense: return launch_mode<kBwdDense>(p, bh, stream);
-    case kBwdMask: return launch_mode<kBwdMask>(p, bh, stream);
-    case kBwdBias: return launch_mode<kBwdBias>(p, bh, stream);
+    case kBwdDense: return launch_mode<kBwdDense>(p, stream);
+    case kBwdMask: return launch_mode<kBwdMask>(p, stream);
+    case kBwdBias: return launch_mode<kBwdBias>(p, stream);
     default: return hipErrorInvalidValue;
   }
 }

@@ -17,11 +17,21 @@ struct BiasParams {
   int n_buckets;
   int n_dist;              // n_q + n_k - 1
   float* by_dist;          // workspace [H][dist_stride]: bias / scale by distance, -inf: closed
-  int32_t* runs;           // workspace [n_runs]: bucket of 32 distances if one, kRunMixed, kRunClosed
+  int32_t* runs;           // workspace [n_runs]: what 32 distances hold, see below
   int dist_stride;         // floats, a multiple of 32
   int n_runs;              // ceil(n_dist / 32)
 };
-enum { kRunClosed = -1, kRunMixed = -2 };
+
+// A word of runs: the bucket of 32 distances that share one (kRunClosed: all closed), kRunMixed,
+// or run_step where the first `pos` of them share one and the rest another.
+enum { kRunClosed = -1, kRunMixed = -2, kRunStep = 1 << 30 };
+constexpr int run_step(int first, int last, int pos) {
+  return kRunStep | pos << 20 | (first + 1) << 10 | (last + 1);
+}
+constexpr bool is_step(int run) { return run >= kRunStep; }
+constexpr int run_first(int run) { return is_step(run) ? (run >> 10 & 1023) - 1 : run; }
+constexpr int run_last(int run) { return is_step(run) ? (run & 1023) - 1 : run; }
+constexpr int run_pos(int run) { return run >> 20 & 1023; }
 constexpr int kMaxBuckets = 512;   // what the backward pass keeps of them in LDS
 
 // Fill by_dist and runs.
@@ -37,7 +47,7 @@ struct BwdParams {
   uint16_t* dq;
   uint16_t* dk;
   uint16_t* dv;
-  int H, n_q, n_k;
+  int bh, H, n_q, n_k;     // bh: batches times heads
   float c;                 // scale * log2(e)
   float scale;
   // workspace, rows padded to n_rows (a multiple of 64)
@@ -58,7 +68,7 @@ struct BwdParams {
 int bwd_padded_rows(int n_q);
 int bwd_key_groups(int n_k);
 
-hipError_t launch_attn_bwd(int mode, const BwdParams& p, int bh, hipStream_t stream);
+hipError_t launch_attn_bwd(int mode, const BwdParams& p, hipStream_t stream);
 
 }  // namespace dsattn
 

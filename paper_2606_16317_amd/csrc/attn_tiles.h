@@ -31,6 +31,7 @@ constexpr int kD = 128;                  // head dimension
 constexpr int kRowBytes = kD * 2;
 constexpr int kTile = 64;                // rows of an LDS tile
 constexpr int kTileElems = kTile * kD;   // 16 KiB
+constexpr int kBlockBytes = 32 * kRowBytes;
 constexpr int kWaves = 4;
 constexpr int kThreads = kWaves * 64;
 
@@ -50,11 +51,24 @@ __device__ __forceinline__ int tile_swz(int row) { return ((row & 3) << 2) | ((r
 // LDS byte address of p.
 __device__ __forceinline__ uint32_t lds_addr(const void* p) { return (uint32_t)(uintptr_t)p; }
 
-// Operand reads take the LDS byte address of a block's first row plus the lane's own part
-// (row_lane, col_lane); what changes from operand to operand is then an XOR with a constant
-// and a constant offset, of which only the XOR takes an instruction and none a register for
-// longer than the read.  here() keeps the compiler from holding all the XORed addresses of a
-// loop in registers instead.
+// Operand reads take the lane's own part of the LDS byte address (row_lane, col_lane; it lies
+// below kBlockBytes), the byte offset `block` of a 32-row block, and constants.  What changes from
+// operand to operand is an XOR with a constant: one instruction.  Where registers are scarce,
+// `block` is the same for the whole wave and part of a scalar XORed value, which leaves no vector
+// register in use between the reads; scalar() keeps the compiler from splitting that XOR and
+// holding the parts in some.  Otherwise (InLane) the lane's part has it already, kept opaque by
+// here(), and the XOR is with a literal, which saves the scalar instructions.
+__device__ __forceinline__ uint32_t scalar(uint32_t x) {
+  x = __builtin_amdgcn_readfirstlane(x);
+  asm volatile("" : "+s"(x));
+  return x;
+}
+__device__ __forceinline__ void here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+struct InLane {};
+__device__ __forceinline__ uint32_t flip(uint32_t at, uint32_t block, uint32_t x) {
+  return at ^ scalar(block | x);
+}
+__device__ __forceinline__ uint32_t flip(uint32_t at, InLane, uint32_t x) { return at ^ x; }
 __device__ __forceinline__ uint32_t row_lane(int r, int g) {
   return (uint32_t)(r * kRowBytes + ((tile_swz(r) ^ g) << 4));
 }
@@ -63,22 +77,25 @@ __device__ __forceinline__ uint32_t col_lane(int lane) {
   return (uint32_t)((4 * g + i) * kRowBytes + (i << 6) +
                     (((2 * (grp & 1) + ((lg & 3) >> 1)) ^ g) << 4) + 8 * (lg & 1));
 }
-__device__ __forceinline__ void here(uint32_t& x) { asm volatile("" : "+v"(x)); }
 
-// Row operand: rows r of the block, k-step s (columns 16 s + 8 g + 0..7).
-__device__ __forceinline__ bf16x8 row_operand(uint32_t at, int offset, int s) {
+// Row operand, of the tiles at LDS address `tiles`: rows r of the block, k-step s (columns 16 s + 8 g + 0..7).
+template <typename BLOCK>
+__device__ __forceinline__ bf16x8 row_operand(uint32_t at, BLOCK block, uint32_t tiles, int s) {
   typedef __attribute__((address_space(3))) const u32x4 lds_u32x4;
-  return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)((at ^ (uint32_t)(s << 5)) + offset));
+  const uint32_t x = flip(at, block, (uint32_t)(s << 5)) + tiles;
+  return __builtin_bit_cast(bf16x8, *(lds_u32x4*)(uintptr_t)x);
 }
 
 // Transposed operand: columns 32 db + r as rows; k-step s (0..1) of the 32-row block, the rows
 // that registers 8 s .. 8 s + 7 of a D block hold.
-__device__ __forceinline__ bf16x8 col_operand(uint32_t at, int offset, int s, int db) {
+template <typename BLOCK>
+__device__ __forceinline__ bf16x8 col_operand(uint32_t at, BLOCK block, uint32_t tiles, int s, int db) {
   typedef __attribute__((address_space(3))) i16x4 lds_i16x4;
   bf16x8 out;
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
-    const uint32_t x = (at ^ (uint32_t)((db << 6) | (c << 5))) + offset + 8 * (2 * s + c) * kRowBytes;
+    const uint32_t x = flip(at, block, (uint32_t)((db << 6) | (c << 5))) + tiles +
+                       8 * (2 * s + c) * kRowBytes;
     const bf16x4 y = __builtin_bit_cast(
         bf16x4, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_i16x4*)(uintptr_t)x));
 #pragma unroll

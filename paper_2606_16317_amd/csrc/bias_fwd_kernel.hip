@@ -146,7 +146,7 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       for (int j = 0; j < 4; ++j) run[j] = __builtin_amdgcn_readfirstlane(sm.runs[buf][3 - w + j]);
 #pragma unroll
       for (int b = 0; b < 2; ++b) {
-        mixed[b] = !(run[b] == run[b + 1] && run[b] == run[b + 2]) || run[b] == kRunMixed;
+        mixed[b] = !(run[b] == run[b + 1] && run[b] == run[b + 2]) || run[b] == kRunMixed || is_step(run[b]);
         tb.flat[b] = mixed[b] ? 0.f : sm.win[buf][32 * b - 32 * w + 127] * p.c;
       }
     };
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       for (int i = 0; i < 8; ++i)
 #pragma unroll
         for (int b = 0; b < 2; ++b) {
-          const bf16x8 a = row_operand(at, b * 32 * kRowBytes, i);
+          const bf16x8 a = row_operand(at, InLane{}, b * kBlockBytes, i);
           s[b] = i == 0 ? first_product(a, qf[0], mixed[b], win_at(0, b)) : mfma(a, qf[i], s[b]);
         }
       const int lim = p.n_k - t0 * kTile - 4 * g;
@@ -201,8 +201,8 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       here(va);
       // operands in the order of their products: 16 of S (key blocks alternating), 16 of P V
       auto operand = [&](int i) {
-        if (i < 16) return row_operand(ka, (i & 1) * 32 * kRowBytes, i >> 1);
-        return col_operand(va, ((i - 16) >> 3) * 32 * kRowBytes, ((i - 16) >> 2) & 1, i & 3);
+        if (i < 16) return row_operand(ka, InLane{}, (i & 1) * kBlockBytes, i >> 1);
+        return col_operand(va, InLane{}, ((i - 16) >> 3) * kBlockBytes, ((i - 16) >> 2) & 1, i & 3);
       };
       f32x16 sn[2];
       float xs[32];

@@ -852,6 +852,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   p.dq = static_cast<uint16_t*>(a.dq);
   p.dk = static_cast<uint16_t*>(a.dk);
   p.dv = static_cast<uint16_t*>(a.dv);
+  p.bh = a.B * a.H;
   p.H = a.H;
   p.n_q = p.n_k = a.N;
   p.c = (float)((double)a.scale * kLog2e);
@@ -867,7 +868,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   p.n_units = n_units;
   p.n_dec = n_dec;
   const hipError_t e = dsattn::launch_attn_bwd(masked ? dsattn::kBwdMask : dsattn::kBwdDense, p,
-                                               a.B * a.H, a.stream);
+                                               a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
   g_last_error.clear();
   return DSATTN_OK;
@@ -1044,6 +1045,7 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.dq = static_cast<uint16_t*>(a.dq);
   p.dk = static_cast<uint16_t*>(a.dk);
   p.dv = static_cast<uint16_t*>(a.dv);
+  p.bh = (int)bh;
   p.H = a.H;
   p.n_q = a.n_q;
   p.n_k = a.n_k;
@@ -1057,7 +1059,7 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.dtable = a.dtable;
   p.dtable_part = static_cast<float*>(
       ws.take(bh * (size_t)dsattn::bwd_key_groups(a.n_k) * (size_t)a.n_buckets * sizeof(float)));
-  const hipError_t e = dsattn::launch_attn_bwd(dsattn::kBwdBias, p, (int)bh, a.stream);
+  const hipError_t e = dsattn::launch_attn_bwd(dsattn::kBwdBias, p, a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
   g_last_error.clear();
   return DSATTN_OK;
