@@ -200,18 +200,6 @@ __device__ __forceinline__ float wave_sum(float x) {
   return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), 63));
 }
 
-// Head and 128-row group of a workgroup.  A bias that closes later keys leaves the first key group
-// and the last query group the most to do: with a bias these come first for all heads, so that no
-// long one starts late.  (Otherwise a head's groups stand together, whose tiles L2 then shares.)
-template <int MODE>
-__device__ __forceinline__ int group_head(const BwdParams& p) {
-  return MODE == kBwdBias ? (int)(blockIdx.x % (unsigned)p.bh) : (int)blockIdx.y;
-}
-template <int MODE>
-__device__ __forceinline__ int group_index(const BwdParams& p) {
-  return MODE == kBwdBias ? (int)(blockIdx.x / (unsigned)p.bh) : (int)blockIdx.x;
-}
-
 // ---- dk, dv ------------------------------------------------------------------------------
 
 // What a workgroup's LDS holds besides tiles.
@@ -442,7 +430,9 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   __shared__ DkvSmem<MODE> sm;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = group_head<MODE>(p), key0 = group_index<MODE>(p) * 128;
+  const int x = blockIdx.x;
+  const Place at = place_of(MODE == kBwdBias, p.dkv_split.unit(x), p.bh, (p.n_k + 127) / 128, false);
+  const int bh = at.bh, key0 = at.group * 128;
   const int n_tiles = (p.n_q + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto qrs = row_buffer(p.q + qoff, p.n_q), grs = row_buffer(p.dout + qoff, p.n_q);
@@ -481,9 +471,13 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     if (tid < 32) sm.side.closed[tid] = neg_inf();
     __syncthreads();
   }
+  int skip, end;
+  p.dkv_split.share(x, count, skip, end);
+  first += skip;
+  count = end - skip;
   auto tile_at = [&](int i) {
     if constexpr (MODE == kBwdMask)
-      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[i]);
+      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[first + i]);
     else
       return first + i;
   };
@@ -508,7 +502,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     if (b == 0) {
       tiles_ready();
       if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
-      if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
+      if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[first + (i >> 1)]);
       if constexpr (MODE == kBwdBias)
         tile.read(sm.side.runs[buf], w, -(first_distance(tile_at(i >> 1)) & 31),
                   &sm.side.win[buf][32 * w + 63], -32);
@@ -537,13 +531,19 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     }
   }
   if (key < p.n_k) {
-    store_row(p.dv + koff, key, dv, 1.f, g);
-    store_row(p.dk + koff, key, dk, p.scale, g);
+    if (x < p.dkv_split.full) {
+      store_row(p.dv + koff, key, dv, 1.f, g);
+      store_row(p.dk + koff, key, dk, p.scale, g);
+    } else {
+      const size_t part = ((size_t)(x - p.dkv_split.full) * part_rows(p.n_k) + (key - key0)) * kD;
+      store_part(p.part_a + part, dk, g);
+      store_part(p.part_b + part, dv, g);
+    }
   }
   if constexpr (MODE == kBwdBias) {
     far.flush(sm.side.bins[w], lane);
     __syncthreads();
-    float* part = p.dtable_part + ((size_t)bh * ((p.n_k + 127) / 128) + key0 / 128) * p.bias.n_buckets;
+    float* part = p.dtable_part + (size_t)x * p.bias.n_buckets;
     for (int i = tid; i < p.bias.n_buckets; i += kThreads)
       part[i] = (sm.side.bins[0][i] + sm.side.bins[1][i]) + (sm.side.bins[2][i] + sm.side.bins[3][i]);
   }
@@ -643,9 +643,9 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   __shared__ DqSmem<MODE> sm;
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int bh = group_head<MODE>(p);
-  const int group = group_index<MODE>(p), n_groups = (p.n_q + 127) / 128;
-  const int q0 = (MODE == kBwdBias ? n_groups - 1 - group : group) * 128;
+  const int x = blockIdx.x;
+  const Place at = place_of(MODE == kBwdBias, p.dq_split.unit(x), p.bh, (p.n_q + 127) / 128, true);
+  const int bh = at.bh, q0 = at.group * 128;
   const int n_tiles = (p.n_k + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
@@ -673,9 +673,13 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     first = sm.side.range.first;
     count = max(0, sm.side.range.last - first + 1);
   }
+  int skip, end;
+  p.dq_split.share(x, count, skip, end);
+  first += skip;
+  count = end - skip;
   auto tile_at = [&](int i) {
     if constexpr (MODE == kBwdMask)
-      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[i]);
+      return (int)__builtin_amdgcn_readfirstlane(sm.side.tile[first + i]);
     else
       return first + i;
   };
@@ -704,7 +708,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       if (b == 0) {
         tiles_ready();
         if (i + 2 < 2 * count) fetch(buf ^ 1, tile_at((i >> 1) + 1));
-        if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[i >> 1]);
+        if constexpr (MODE == kBwdMask) bits = __builtin_amdgcn_readfirstlane(sm.side.bits[first + (i >> 1)]);
         if constexpr (MODE == kBwdBias)
           tile.read(sm.side.runs[buf], 3 - w, 0, &sm.side.win[buf][127 - 32 * w], 32);
       }
@@ -727,6 +731,16 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   visit_blocks(std::false_type{}, 0, ragged ? 2 * count - 2 : 2 * count);
   if (ragged) visit_blocks(std::true_type{}, 2 * count - 2, 2 * count);
   const float exact = half_sum(delta + rest), off_by = exact + nd;
+  if (x >= p.dq_split.full) {
+    if (row < p.n_q) {
+      const int slot = x - p.dq_split.full;
+      const size_t part = ((size_t)slot * part_rows(p.n_q) + (row - q0)) * kD;
+      store_part(p.part_a + part, dq, g);
+      store_part(p.part_b + part, pk, g);
+      if (g == 0) p.part_delta[(size_t)slot * 128 + (row - q0)] = exact;
+    }
+    return;
+  }
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
@@ -735,6 +749,52 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     store_row(p.dq + qoff, row, dq, p.scale, g);
     if (g == 0) p.neg_delta[(size_t)bh * p.n_rows + row] = -exact;
   }
+}
+
+// ---- joins -------------------------------------------------------------------------------
+
+// Sum of a shared unit's parts in their order, 4 columns of one row; slot0: the first part's slot.
+__device__ __forceinline__ f32x4 sum_parts(const float* part, const WorkSplit& split, int slot0,
+                                           int rows, int row, int col) {
+  f32x4 x = f32x4{};
+  for (int j = 0; j < split.parts; ++j)
+    x += *reinterpret_cast<const f32x4*>(
+        part + ((size_t)(slot0 + j * split.shared()) * rows + row) * kD + col);
+  return x;
+}
+
+// dq and delta, as at the end of bwd_dq_kernel.  32 lanes a row.
+__global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias) {
+  const int rows = part_rows(p.n_q), col = 4 * (threadIdx.x & 31);
+  const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
+  if (slot0 >= p.dq_split.shared()) return;
+  const Place at = place_of(bias, p.dq_split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
+  const int row = at.group * 128 + local;
+  if (row >= p.n_q) return;
+  float exact = 0.f;
+  for (int j = 0; j < p.dq_split.parts; ++j)
+    exact += p.part_delta[(size_t)(slot0 + j * p.dq_split.shared()) * 128 + local];
+  float* nd = p.neg_delta + (size_t)at.bh * p.n_rows + row;
+  const float off_by = exact + *nd;
+  f32x4 x = sum_parts(p.part_a, p.dq_split, slot0, rows, local, col);
+  const f32x4 y = sum_parts(p.part_b, p.dq_split, slot0, rows, local, col);
+#pragma unroll
+  for (int t = 0; t < 4; ++t) x[t] = fmaf(-off_by, y[t], x[t]);
+  store_cols(p.dq + ((size_t)at.bh * p.n_q + row) * kD + col, x, p.scale);
+  __builtin_amdgcn_wave_barrier();   // the row's lanes, all of one wave, have read it
+  if (col == 0) *nd = -exact;
+}
+
+__global__ __launch_bounds__(256) void bwd_join_dkv_kernel(BwdParams p, bool bias) {
+  const int rows = part_rows(p.n_k), col = 4 * (threadIdx.x & 31);
+  const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
+  if (slot0 >= p.dkv_split.shared()) return;
+  const Place at = place_of(bias, p.dkv_split.full + slot0, p.bh, (p.n_k + 127) / 128, false);
+  const int row = at.group * 128 + local;
+  if (row >= p.n_k) return;
+  const size_t out = ((size_t)at.bh * p.n_k + row) * kD + col;
+  store_cols(p.dk + out, sum_parts(p.part_a, p.dkv_split, slot0, rows, local, col), p.scale);
+  store_cols(p.dv + out, sum_parts(p.part_b, p.dkv_split, slot0, rows, local, col), 1.f);
 }
 
 // ---- the bias by distance, and the table's gradient -----------------------------------------
@@ -761,16 +821,21 @@ __global__ __launch_bounds__(256) void bias_prepare_kernel(BiasParams b, int H, 
   }
 }
 
-// dtable[i][h]: the parts of all batches and key groups, in 64 bits and a fixed order.  Lane i of
-// every wave takes bucket i, the 16 waves share the parts.
+// dtable[i][h]: the parts of all workgroups of the head, in 64 bits and a fixed order.  Lane i of
+// every wave takes bucket i, the 16 waves share the units.
 __global__ __launch_bounds__(1024) void bias_dtable_kernel(BwdParams p, int B, int groups) {
   __shared__ double sum[16][64];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, h = blockIdx.y;
   const int i = blockIdx.x * 64 + lane, n = p.bias.n_buckets;
+  const WorkSplit& split = p.dkv_split;
   double x = 0.0;
   if (i < n)
-    for (int j = w; j < B * groups; j += 16)
-      x += p.dtable_part[((size_t)(j / groups * p.H + h) * groups + j % groups) * n + i];
+    for (int j = w; j < B * groups; j += 16) {
+      const int unit = j / B * p.bh + j % B * p.H + h;   // see place_of
+      const int parts = unit < split.full ? 1 : split.parts;
+      for (int k = 0; k < parts; ++k)
+        x += p.dtable_part[(size_t)(unit + k * split.shared()) * n + i];
+    }
   sum[w][lane] = x;
   __syncthreads();
   if (w == 0 && i < n) {
@@ -782,29 +847,39 @@ __global__ __launch_bounds__(1024) void bias_dtable_kernel(BwdParams p, int B, i
 // (Without queries, keys or batches, which only a bias call passes on, the rest still runs.)
 template <int MODE>
 hipError_t launch_mode(const BwdParams& p, hipStream_t stream) {
-  const int bh = p.bh;
-  auto grid = [&](int n) { return MODE == kBwdBias ? dim3((unsigned)n * bh) : dim3(n, bh); };
-  if (MODE == kBwdBias) {
+  constexpr bool bias = MODE == kBwdBias;
+  const dim3 block(kThreads);
+  auto joined = [](const WorkSplit& s, int n) { return dim3((s.shared() * part_rows(n) + 7) / 8); };
+  if (bias) {
     const hipError_t e = launch_bias_prepare(p.bias, p.H, p.scale, stream);
     if (e != hipSuccess) return e;
   }
-  if (bh > 0 && p.n_q > 0) {
-    hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, bh), dim3(256), 0, stream, p);
-    hipLaunchKernelGGL((bwd_dq_kernel<MODE>), grid((p.n_q + 127) / 128), dim3(kThreads), 0, stream, p);
+  if (p.bh > 0 && p.n_q > 0) {
+    hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, p.bh), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((bwd_dq_kernel<MODE>), dim3(p.dq_split.grid()), block, 0, stream, p);
+    if (p.dq_split.shared() > 0)
+      hipLaunchKernelGGL(bwd_join_dq_kernel, joined(p.dq_split, p.n_q), dim3(256), 0, stream, p, bias);
   }
-  const int groups = bwd_key_groups(p.n_k);
-  if (bh > 0 && groups > 0)
-    hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), grid(groups), dim3(kThreads), 0, stream, p);
-  if (MODE == kBwdBias)
+  if (p.bh > 0 && p.n_k > 0) {
+    hipLaunchKernelGGL((bwd_dkv_kernel<MODE>), dim3(p.dkv_split.grid()), block, 0, stream, p);
+    if (p.dkv_split.shared() > 0)
+      hipLaunchKernelGGL(bwd_join_dkv_kernel, joined(p.dkv_split, p.n_k), dim3(256), 0, stream, p, bias);
+  }
+  if (bias)
     hipLaunchKernelGGL(bias_dtable_kernel, dim3((p.bias.n_buckets + 63) / 64, p.H), dim3(1024), 0,
-                       stream, p, bh / p.H, groups);
+                       stream, p, p.bh / p.H, (p.n_k + 127) / 128);
   return hipGetLastError();
 }
 
 }  // namespace
 
 int bwd_padded_rows(int n_q) { return (n_q + kTile - 1) / kTile * kTile; }
-int bwd_key_groups(int n_k) { return (n_k + 127) / 128; }
+
+// A part's 128 KiB of sums are written and read at about 4.5 TB/s, 0.06 us; a tile takes 3.5 us.
+WorkSplit bwd_split(int bh, int n_own, int n_streamed) {
+    return make_split((long long)bh * ((n_own + 127) / 128), (n_streamed + kTile - 1) / kTile,
+                    0.017 * part_rows(n_own) / 128);
+}
 
 hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream) {
   if (b.n_dist == 0) return hipSuccess;

@@ -2,6 +2,8 @@
 #ifndef DSATTN_ATTN_BWD_LAUNCH_H
 #define DSATTN_ATTN_BWD_LAUNCH_H
 
+#include "attn_split.h"
+
 #include <hip/hip_runtime_api.h>
 #include <stddef.h>
 #include <stdint.h>
@@ -54,6 +56,11 @@ struct BwdParams {
   float* neg_lse2;         // [BH][n_rows]: -lse * log2(e); -inf for rows that saw no key or do not exist
   float* neg_delta;        // [BH][n_rows]: -(dO . O), then in bias mode -(sum of P dP)
   int n_rows;
+  // units of the dq and of the dk, dv kernel, and the partial results of units that are shared
+  WorkSplit dq_split, dkv_split;
+  float* part_a;           // [slots][min(n, 128)][128]: sums of dS K, later of dS^T Q
+  float* part_b;           // of P K, later of P^T dO
+  float* part_delta;       // [slots][128]
   // kBwdMask
   const uint8_t* mask;     // [BH][n_units][n_dec], nonzero: skipped
   int tile_q, tile_k;
@@ -61,12 +68,14 @@ struct BwdParams {
   // kBwdBias
   BiasParams bias;
   float* dtable;           // [n_buckets][H]
-  float* dtable_part;      // workspace [BH][n_key_groups][n_buckets]
+  float* dtable_part;      // workspace [dkv_split.grid()][n_buckets]
 };
 
-// Rows of a head's padded per-row workspace, and key groups (workgroups of the dk, dv kernel).
+// Rows of a head's padded per-row workspace.
 int bwd_padded_rows(int n_q);
-int bwd_key_groups(int n_k);
+
+// The launches' units.
+WorkSplit bwd_split(int bh, int n_own, int n_streamed);
 
 hipError_t launch_attn_bwd(int mode, const BwdParams& p, hipStream_t stream);
 

@@ -204,6 +204,24 @@ __device__ __forceinline__ void store_row(uint16_t* base, int row, const f32x16 
     }
 }
 
+// Store a^T as one row of partial sums.
+__device__ __forceinline__ void store_part(float* row, const f32x16 (&a)[4], int g) {
+#pragma unroll
+  for (int db = 0; db < 4; ++db)
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      *reinterpret_cast<f32x4*>(row + 32 * db + 8 * i + 4 * g) =
+          f32x4{a[db][4 * i], a[db][4 * i + 1], a[db][4 * i + 2], a[db][4 * i + 3]};
+}
+
+// Store four columns of a row of sums, times m, as bf16.
+__device__ __forceinline__ void store_cols(uint16_t* out, const f32x4& x, float m) {
+  bf16x4 h;
+#pragma unroll
+  for (int t = 0; t < 4; ++t) h[t] = (__bf16)(x[t] * m);
+  *reinterpret_cast<bf16x4*>(out) = h;
+}
+
 }  // namespace
 }  // namespace dsattn
 

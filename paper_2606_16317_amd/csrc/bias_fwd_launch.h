@@ -16,15 +16,16 @@ struct BiasFwdParams {
   float c;                 // scale * log2(e)
   float scale;
   BiasParams bias;
-  int splits;              // workgroups that share the keys of a query tile
-  float* part_o;           // workspace [splits][BH][n_q][128], or null for one split
-  float* part_ml;          // workspace [splits][BH][n_q][2]: reference maximum (log2) and row sum
+  int bh;                  // batches times heads
+  WorkSplit split;
+  float* part_o;           // workspace [slots][min(n_q, 128)][128]
+  float* part_ml;          // workspace [slots][128][2]: reference maximum (log2) and row sum
 };
 
-// Parts that a problem's keys are split into.
-int bias_fwd_splits(int bh, int n_q, int n_k);
+// The launch's units.
+WorkSplit bias_fwd_split(int bh, int n_q, int n_k);
 
-hipError_t launch_bias_fwd(const BiasFwdParams& p, int bh, hipStream_t stream);
+hipError_t launch_bias_fwd(const BiasFwdParams& p, hipStream_t stream);
 
 }  // namespace dsattn
 

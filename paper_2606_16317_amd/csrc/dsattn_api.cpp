@@ -793,15 +793,47 @@ size_t bwd_rows_bytes(int B, int H, int n) {
   return 2 * round_up((size_t)B * (size_t)H * (size_t)dsattn::bwd_padded_rows(n) * sizeof(float));
 }
 
+// Bytes of one of the two arrays of partial sums; the dq and the dk, dv kernel use them in turn.
+size_t bwd_part_bytes(int bh, int n_q, int n_k) {
+  const auto floats = [](const dsattn::WorkSplit& s, int n) {
+    return (size_t)s.slots() * (size_t)dsattn::part_rows(n) * kHeadDim;
+  };
+  return round_up(std::max(floats(dsattn::bwd_split(bh, n_q, n_k), n_q),
+                           floats(dsattn::bwd_split(bh, n_k, n_q), n_k)) * sizeof(float));
+}
+
+size_t bwd_delta_bytes(int bh, int n_q, int n_k) {
+  return round_up((size_t)dsattn::bwd_split(bh, n_q, n_k).slots() * 128 * sizeof(float));
+}
+
+size_t bwd_bytes(int B, int H, int n_q, int n_k) {
+  return bwd_rows_bytes(B, H, n_q) + 2 * bwd_part_bytes(B * H, n_q, n_k) +
+         bwd_delta_bytes(B * H, n_q, n_k);
+}
+
+// What both backward calls fill in alike, n_q and n_k set before.
+void bwd_slices(dsattn::BwdParams& p, Slices& ws) {
+  p.n_rows = dsattn::bwd_padded_rows(p.n_q);
+  const size_t row_bytes = (size_t)p.bh * (size_t)p.n_rows * sizeof(float);
+  p.neg_lse2 = static_cast<float*>(ws.take(row_bytes));
+  p.neg_delta = static_cast<float*>(ws.take(row_bytes));
+  p.dq_split = dsattn::bwd_split(p.bh, p.n_q, p.n_k);
+  p.dkv_split = dsattn::bwd_split(p.bh, p.n_k, p.n_q);
+  p.part_a = static_cast<float*>(ws.take(bwd_part_bytes(p.bh, p.n_q, p.n_k)));
+  p.part_b = static_cast<float*>(ws.take(bwd_part_bytes(p.bh, p.n_q, p.n_k)));
+  p.part_delta = static_cast<float*>(ws.take(bwd_delta_bytes(p.bh, p.n_q, p.n_k)));
+}
+
 bool sane_extents(int B, int H, int n) {
   return B > 0 && H > 0 && n > 0 && (long long)B * H <= 65535 &&
-         (long long)n * kHeadDim * 2 <= INT32_MAX;
+         (long long)n * kHeadDim * 2 <= INT32_MAX &&
+         (long long)n * kHeadDim * B * H <= (1LL << 40);
 }
 
 }  // namespace
 
 size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N) {
-  return sane_extents(B, H, N) ? bwd_rows_bytes(B, H, N) : 0;
+  return sane_extents(B, H, N) ? bwd_bytes(B, H, N, N) : 0;
 }
 
 int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_size) {
@@ -825,7 +857,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
     g_last_error.clear();
     return DSATTN_OK;
   }
-  const size_t need = bwd_rows_bytes(a.B, a.H, a.N);
+  const size_t need = bwd_bytes(a.B, a.H, a.N, a.N);
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t rows = (size_t)a.B * (size_t)a.H * (size_t)a.N, wide = rows * kHeadDim * 2;
   const int n_units = (a.N + a.tile_q - 1) / a.tile_q, n_dec = (a.N + a.tile_k - 1) / a.tile_k;
@@ -858,10 +890,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   p.c = (float)((double)a.scale * kLog2e);
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
-  p.n_rows = dsattn::bwd_padded_rows(a.N);
-  const size_t row_floats = (size_t)a.B * (size_t)a.H * (size_t)p.n_rows * sizeof(float);
-  p.neg_lse2 = static_cast<float*>(ws.take(row_floats));
-  p.neg_delta = static_cast<float*>(ws.take(row_floats));
+  bwd_slices(p, ws);
   p.mask = masked ? a.mask_in : nullptr;
   p.tile_q = a.tile_q;
   p.tile_k = a.tile_k;
@@ -922,15 +951,15 @@ dsattn::BiasParams bias_params(const float* table, const int32_t* bucket, int n_
 }
 
 size_t bias_fwd_bytes(int B, int H, int n_q, int n_k) {
-  const size_t splits = (size_t)dsattn::bias_fwd_splits(B * H, n_q, n_k);
-  const size_t rows = splits == 1 ? 0 : splits * (size_t)B * (size_t)H * (size_t)n_q;
-  return bias_layout_bytes(H, n_q, n_k) + round_up(rows * kHeadDim * sizeof(float)) +
-         round_up(rows * 2 * sizeof(float));
+  const size_t slots = (size_t)dsattn::bias_fwd_split(B * H, n_q, n_k).slots();
+  return bias_layout_bytes(H, n_q, n_k) +
+         round_up(slots * (size_t)dsattn::part_rows(n_q) * kHeadDim * sizeof(float)) +
+         round_up(slots * 128 * 2 * sizeof(float));
 }
 
 size_t bias_bwd_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
-  const size_t parts = (size_t)B * (size_t)H * (size_t)dsattn::bwd_key_groups(n_k);
-  return bias_layout_bytes(H, n_q, n_k) + bwd_rows_bytes(B, H, n_q) +
+  const size_t parts = (size_t)dsattn::bwd_split(B * H, n_k, n_q).grid();
+  return bias_layout_bytes(H, n_q, n_k) + bwd_bytes(B, H, n_q, n_k) +
          round_up(parts * (size_t)n_buckets * sizeof(float));
 }
 
@@ -988,13 +1017,13 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
   p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
-  p.splits = dsattn::bias_fwd_splits((int)bh, a.n_q, a.n_k);
-  if (p.splits > 1) {
-    const size_t rows = (size_t)p.splits * bh * (size_t)a.n_q;
-    p.part_o = static_cast<float*>(ws.take(rows * kHeadDim * sizeof(float)));
-    p.part_ml = static_cast<float*>(ws.take(rows * 2 * sizeof(float)));
-  }
-  const hipError_t e = dsattn::launch_bias_fwd(p, (int)bh, a.stream);
+  p.bh = (int)bh;
+  p.split = dsattn::bias_fwd_split(p.bh, a.n_q, a.n_k);
+  const size_t slots = (size_t)p.split.slots();
+  p.part_o = static_cast<float*>(
+      ws.take(slots * (size_t)dsattn::part_rows(a.n_q) * kHeadDim * sizeof(float)));
+  p.part_ml = static_cast<float*>(ws.take(slots * 128 * 2 * sizeof(float)));
+  const hipError_t e = dsattn::launch_bias_fwd(p, a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
   g_last_error.clear();
   return DSATTN_OK;
@@ -1053,12 +1082,10 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
   p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
-  p.n_rows = dsattn::bwd_padded_rows(a.n_q);
-  p.neg_lse2 = static_cast<float*>(ws.take(bh * (size_t)p.n_rows * sizeof(float)));
-  p.neg_delta = static_cast<float*>(ws.take(bh * (size_t)p.n_rows * sizeof(float)));
+  bwd_slices(p, ws);
   p.dtable = a.dtable;
   p.dtable_part = static_cast<float*>(
-      ws.take(bh * (size_t)dsattn::bwd_key_groups(a.n_k) * (size_t)a.n_buckets * sizeof(float)));
+      ws.take((size_t)p.dkv_split.grid() * (size_t)a.n_buckets * sizeof(float)));
   const hipError_t e = dsattn::launch_attn_bwd(dsattn::kBwdBias, p, a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
   g_last_error.clear();
