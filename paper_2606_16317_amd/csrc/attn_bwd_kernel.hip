@@ -208,7 +208,6 @@ struct DkvBias {
   alignas(16) float win[2][kWindow];       // bias / scale
   alignas(16) int32_t bucket[2][kWindow];
   int32_t runs[2][64];
-  float diag[kWaves][2][64];               // sums over a block's distances, per lane half
   float bins[kWaves][kMaxBuckets];         // sums over buckets
   float closed[32];                        // -inf, read by lanes whose key does not exist
   TileRange range;
@@ -253,6 +252,35 @@ __device__ __forceinline__ void lds_add(float* p, float x) {
   __hip_atomic_fetch_add(p, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
 }
 
+// Sums of a 32 x 32 block over its diagonals: lane l gets that of the block's l-th smallest
+// column - row distance.  Row after row is added to what came before, moved on by one lane, so
+// that row i ends 31 - i lanes on.  (32 additions that read their neighbour's lane.  Adding up in
+// LDS took 16 atomics of a wave, some 200 cycles each.)
+__device__ __forceinline__ float diagonal_sums(const f32x16& s) {
+  float x = 0.f;
+  const auto add = [&](uint32_t row) {   // 0x138: a lane reads the one below, the first reads 0
+    x = __builtin_bit_cast(float, row) +
+        __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x138,
+                                                              0xf, 0xf, true));
+  };
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    uint32_t upper[4];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      // rows of 32 lanes each in 64: 8 i + t, then 8 i + 4 + t
+      const float y = s[4 * i + t];   // (a bit cast of the element itself takes the vector's first)
+      const auto sw = __builtin_amdgcn_permlane32_swap(__builtin_bit_cast(uint32_t, y), 0u, false,
+                                                       false);
+      add(sw[0]);
+      upper[t] = sw[1];
+    }
+#pragma unroll
+    for (int t = 0; t < 4; ++t) add(upper[t]);
+  }
+  return x;
+}
+
 // Register v's row, 8 (v / 4) + v % 4, counted back from the last one's.
 __device__ __forceinline__ constexpr int back(int v) { return 27 - 8 * (v >> 2) - (v & 3); }
 
@@ -271,16 +299,17 @@ __device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uin
   f32x16 s = f32x16{}, dp, nd;
   if constexpr (MODE == kBwdBias) {
     if (!is_flat(bias.run)) {
-      const float* win = there ? bias.win + 4 + (lane & 31) - 4 * g : sm.side.closed;
+      const int l = lane_now();
+      const float* win = there ? bias.win + 4 + (l & 31) - 4 * (l >> 5) : sm.side.closed;
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = win[back(v)];
+      asm volatile("" : "+v"(s));   // put in order here, not where both ways meet
     } else {
       const float flat = there ? bias.flat : neg_inf();
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = flat;
     }
   }
-  float sum = 0.f;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const f32x4 x = *reinterpret_cast<const f32x4*>(&sm.nd[buf][32 * b + 8 * i + 4 * g]);
@@ -305,10 +334,7 @@ __device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uin
   auto grad = [&](int v) {
     const float x = s[v] * dp[v];
     df[v >> 3][v & 7] = (__bf16)x;
-    if constexpr (MODE == kBwdBias) {
-      sum += x;
-      s[v] = x;
-    }
+    if constexpr (MODE == kBwdBias) s[v] = x;
   };
   constexpr int RK = 3;
   bf16x8 a[RK];
@@ -336,80 +362,65 @@ __device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uin
       if (i >= 16 && i < 20 && e < 1) prob(i - 4);
       if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
-    // dS in 32 bits, now in s, while it is there: of a mixed block by distance, of one with a
-    // step the part below it; the sum of all of it comes from grad
+    // dS in 32 bits, now in s: its sum under the dK products
     if constexpr (MODE == kBwdBias) {
-      if (i == 23) {
-        below = 0.f;
-        if (is_step(bias.run)) {
-          const int cut = run_pos(bias.run) - bias.first - 4 - (lane & 31) + 4 * g;
-#pragma unroll
-          for (int v = 0; v < 16; ++v) below += back(v) < cut ? s[v] : 0.f;
-        } else if (bias.run == kRunMixed) {
-          float* diag = &sm.side.diag[w][g][(lane & 31) + 4 - 4 * g];
-#pragma unroll
-          for (int v = 0; v < 16; ++v) lds_add(diag + back(v), s[v]);
-        }
-      }
+      if (i == 24) all = s[0] + s[1];
+      if (i > 24) all += s[2 * (i - 24)] + s[2 * (i - 24) + 1];
     }
     sched_fence();
   }
-  all = sum;
+  // of a mixed block its sums by distance instead, of one with a step the parts above and below it
+  if constexpr (MODE == kBwdBias) {
+    if (is_step(bias.run)) {
+      // (not one of them as a difference: where a part's dS are zeros, so is its sum)
+      const int l = lane_now(), cut = run_pos(bias.run) - bias.first - 4 - (l & 31) + 4 * (l >> 5);
+      all = below = 0.f;
+#pragma unroll
+      for (int v = 0; v < 16; ++v) {
+        below += back(v) < cut ? s[v] : 0.f;
+        all += back(v) < cut ? 0.f : s[v];
+      }
+    } else if (bias.run == kRunMixed) {
+      all = diagonal_sums(s);
+    }
+  }
 }
 
-// Sums over block elements that are not in the bins yet: of two buckets, since blocks come by
-// descending distance and one with a step is followed by others with the same, until one lies
-// below it.  A lane's part is a sum of block sums of 16, the bins take sums of at most 64 blocks:
-// errors grow with the root of each count.
-struct FarSums {
-  int run = kRunClosed, next = kRunClosed;
-  float x = 0.f, y = 0.f;   // of run and of next
-  __device__ __forceinline__ static void put(float* bins, int run, float x, int lane) {
+// Sum over block elements of one bucket that is not in the bins yet: blocks come by descending
+// distance, so most have the bucket of the one before.  A lane's part is a sum of block sums of 16,
+// the bins take sums of at most 64 blocks: errors grow with the root of each count.
+struct FarSum {
+  int run = kRunClosed;
+  float x = 0.f;
+  __device__ __forceinline__ static void put(float* bins, int run, float x) {
     const float total = wave_sum(x);
-    if (lane == 0 && run >= 0) lds_add(&bins[run], total);
+    if (lane_now() == 0 && run >= 0) lds_add(&bins[run], total);
   }
-  __device__ __forceinline__ void flush(float* bins, int lane) {
-    put(bins, run, x, lane);
-    put(bins, next, y, lane);
-    run = next = kRunClosed;
-    x = y = 0.f;
+  __device__ __forceinline__ void flush(float* bins) {
+    put(bins, run, x);
+    run = kRunClosed;
+    x = 0.f;
   }
-  // One block's sums: `all` of it, and what lies below its step.
-  __device__ __forceinline__ void add(float* bins, int block, float all, float below, int lane) {
-    if (block == run) {   // nearly always
-      x += all;
-      return;
+  // One block's sum, or its sums above and below its step.
+  __device__ __forceinline__ void add(float* bins, int block, float all, float below) {
+    if (block != run) {   // seldom
+      const int high = run_last(block);
+      if (high != run) {
+        flush(bins);
+        run = high;
+      }
+      if (is_step(block)) put(bins, run_first(block), below);
     }
-    const int high = run_last(block), low = run_first(block);
-    if (high == next) {   // the step lies behind
-      put(bins, run, x, lane);
-      run = next;
-      x = y;
-      next = kRunClosed;
-      y = 0.f;
-    }
-    if (high != run || (low != high && next != kRunClosed && next != low)) {
-      flush(bins, lane);
-      run = high;
-    }
-    x += all - below;
-    if (low != high) {
-      next = low;
-      y += below;
-    }
+    x += all;
   }
 };
 
-// Add a mixed block's sums by distance to their buckets, and clear them.  All of it is one
-// wave's: its LDS accesses run in order.  A bucket that many of the distances share is summed up
-// first: atomics on one address wait for each other.
-__device__ __forceinline__ void flush_diag(float (&diag)[2][64], const int32_t* bucket, float* bins,
-                                           int n_buckets, int lane) {
-  asm volatile("" ::: "memory");
-  const float x = diag[0][lane] + diag[1][lane];
+// Add a mixed block's sums by distance, x, to their buckets.  A bucket that many of the distances
+// share is summed up first: atomics on one address wait for each other.
+__device__ __forceinline__ void add_by_distance(float x, const int32_t* bucket, float* bins,
+                                                int n_buckets) {
+  const int lane = lane_now();
   int at = bucket[lane];
-  diag[0][lane] = 0.f;
-  diag[1][lane] = 0.f;
   if (lane == 63 || (uint32_t)at >= (uint32_t)n_buckets) at = kRunClosed;
   // the ends of the range are where wide buckets are
 #pragma unroll
@@ -422,7 +433,6 @@ __device__ __forceinline__ void flush_diag(float (&diag)[2][64], const int32_t* 
     }
   }
   if (at >= 0) lds_add(&bins[at], x);
-  asm volatile("" ::: "memory");
 }
 
 template <int MODE>
@@ -438,22 +448,24 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   const auto qrs = row_buffer(p.q + qoff, p.n_q), grs = row_buffer(p.dout + qoff, p.n_q);
   const auto lrs = word_buffer(p.neg_lse2 + (size_t)bh * p.n_rows, p.n_rows);
   const auto drs = word_buffer(p.neg_delta + (size_t)bh * p.n_rows, p.n_rows);
-  const uint32_t off = tile_lane_offset(w, lane);
   const uint32_t row_at = row_lane(r, g), col_at = col_lane(lane);
   const auto first_distance = [&](int t) { return key0 - (t * kTile + 63) + p.n_q - 1; };
   const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
   const auto brs = word_buffer(p.bias.bucket, p.bias.n_dist), rrs = word_buffer(p.bias.runs, p.bias.n_runs);
 
+  const uint32_t off = tile_lane_offset(w, lane);
   auto fetch = [&](int buf, int t) {
-    load_tile(sm.q[buf], qrs, off, t * kTile, w);
-    load_tile(sm.g[buf], grs, off, t * kTile, w);
-    if (w == 0) load_words(sm.nl[buf], lrs, t * kTile, lane);
-    if (w == 1) load_words(sm.nd[buf], drs, t * kTile, lane);
+    const int l = MODE == kBwdBias ? lane_now() : lane;
+    const uint32_t at = MODE == kBwdBias ? tile_lane_offset(w, l) : off;
+    load_tile(sm.q[buf], qrs, at, t * kTile, w);
+    load_tile(sm.g[buf], grs, at, t * kTile, w);
+    if (w == 0) load_words(sm.nl[buf], lrs, t * kTile, l);
+    if (w == 1) load_words(sm.nd[buf], drs, t * kTile, l);
     if constexpr (MODE == kBwdBias) {
       const int e = first_distance(t);
-      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, lane);
-      if (w > 0) load_words(sm.side.bucket[buf] + 64 * (w - 1), brs, e + 64 * (w - 1), lane);
-      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, lane);
+      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, l);
+      if (w > 0) load_words(sm.side.bucket[buf] + 64 * (w - 1), brs, e + 64 * (w - 1), l);
+      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, l);
     }
   };
 
@@ -467,7 +479,6 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     first = sm.side.range.first;
     count = max(0, sm.side.range.last - first + 1);
     for (int i = tid; i < kWaves * kMaxBuckets; i += kThreads) sm.side.bins[0][i] = 0.f;
-    for (int i = tid; i < kWaves * 128; i += kThreads) sm.side.diag[0][0][i] = 0.f;
     if (tid < 32) sm.side.closed[tid] = neg_inf();
     __syncthreads();
   }
@@ -485,7 +496,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   if (count > 0) fetch(0, tile_at(0));
   bf16x8 kf[8], vf[8];
   f32x16 dk[4], dv[4];
-  const int key = key0 + w * 32 + r;
+  int key = key0 + w * 32 + r;
   load_row(kf, p.k + koff, key, key < p.n_k, g);
   load_row(vf, p.v + koff, key, key < p.n_k, g);
 #pragma unroll
@@ -494,9 +505,10 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   // one loop over the 32-row halves: with a loop over tiles around one over their halves the
   // compiler moves all accumulators between the loops
   const bool own = key0 + 32 * w < p.n_k;   // this wave has a key
+  const bool there = key < p.n_k;
   uint32_t bits = 0xffu;
   TileRuns tile{};
-  FarSums far;
+  FarSum far;
   for (int i = 0; i < 2 * count; ++i) {
     const int buf = i >> 1 & 1, b = i & 1;
     if (b == 0) {
@@ -519,18 +531,19 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     }
     float all = 0.f, below = 0.f;
     if (visit)
-      dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, lane, w, key < p.n_k, bias,
+      dkv_block<MODE>(sm, buf, b, row_at, col_at, kf, vf, dk, dv, p.c, lane, w, there, bias,
                       all, below);
     if constexpr (MODE == kBwdBias) {
       if (visit && bias.run == kRunMixed)
-        flush_diag(sm.side.diag[w], &sm.side.bucket[buf][bias.first], sm.side.bins[w],
-                   p.bias.n_buckets, lane);
+        add_by_distance(all, &sm.side.bucket[buf][bias.first], sm.side.bins[w], p.bias.n_buckets);
       else if (visit)
-        far.add(sm.side.bins[w], bias.run, all, below, lane);
-      if ((i & 63) == 63) far.flush(sm.side.bins[w], lane);
+        far.add(sm.side.bins[w], bias.run, all, below);
+      if ((i & 63) == 63) far.flush(sm.side.bins[w]);
     }
   }
+  key = key0 + w * 32 + (lane_now() & 31);
   if (key < p.n_k) {
+    const int g = lane_now() >> 5;
     if (x < p.dkv_split.full) {
       store_row(p.dv + koff, key, dv, 1.f, g);
       store_row(p.dk + koff, key, dk, p.scale, g);
@@ -541,7 +554,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     }
   }
   if constexpr (MODE == kBwdBias) {
-    far.flush(sm.side.bins[w], lane);
+    far.flush(sm.side.bins[w]);
     __syncthreads();
     float* part = p.dtable_part + (size_t)x * p.bias.n_buckets;
     for (int i = tid; i < p.bias.n_buckets; i += kThreads)
@@ -571,14 +584,14 @@ template <int MODE, bool TAIL>
 __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint32_t row_at, uint32_t col_at,
                                          const bf16x8 (&qf)[8], const bf16x8 (&gf)[8],
                                          f32x16 (&dq)[4], f32x16 (&pk)[4], float nl, float nd,
-                                         float c, int lane, int left,
-                                         int run, float flat, const float* win, float& delta, float& rest) {
+                                         float c, int left, int run, float flat, const float* win, float& delta, float& rest) {
   const uint32_t k_at = lds_addr(sm.k), v_at = lds_addr(sm.v);
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
   f32x16 s = f32x16{}, dp;
   if constexpr (MODE == kBwdBias) {
     if (!is_flat(run)) {
-      const float* at = win + 4 * (lane >> 5) - (lane & 31);
+      const int l = lane_now();
+      const float* at = win + 4 * (l >> 5) - (l & 31);
 #pragma unroll
       for (int v = 0; v < 16; ++v) s[v] = at[27 - back(v)];
     } else {
@@ -620,9 +633,10 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       dq[i & 3] = mfma(x, df[(i & 7) >> 2], dq[i & 3]);
     // keys past the end: their rows are zeros, but exp2(-lse) may be infinite
     if (TAIL && i == 8) {
+      const int l = lane_now();
 #pragma unroll
       for (int v = 0; v < 16; ++v)
-        if (27 - back(v) + 4 * (lane >> 5) >= left) s[v] = neg_inf();
+        if (27 - back(v) + 4 * (l >> 5) >= left) s[v] = neg_inf();
     }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {   // as in dkv_block
@@ -649,18 +663,20 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const int n_tiles = (p.n_k + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
   const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
-  const uint32_t off = tile_lane_offset(w, lane);
   const uint32_t row_at = row_lane(r, g), col_at = col_lane(lane);
   const auto first_distance = [&](int t) { return t * kTile - (q0 + 127) + p.n_q - 1; };
   const auto wrs = word_buffer(p.bias.by_dist + (size_t)(MODE == kBwdBias ? bh % p.H : 0) * p.bias.dist_stride, p.bias.n_dist);
   const auto rrs = word_buffer(p.bias.runs, p.bias.n_runs);
+  const uint32_t off = tile_lane_offset(w, lane);
   auto fetch = [&](int buf, int t) {
-    load_tile(sm.k[buf], krs, off, t * kTile, w);
-    load_tile(sm.v[buf], vrs, off, t * kTile, w);
+    const int l = MODE == kBwdBias ? lane_now() : lane;
+    const uint32_t at = MODE == kBwdBias ? tile_lane_offset(w, l) : off;
+    load_tile(sm.k[buf], krs, at, t * kTile, w);
+    load_tile(sm.v[buf], vrs, at, t * kTile, w);
     if constexpr (MODE == kBwdBias) {
       const int e = first_distance(t);
-      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, lane);
-      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, lane);
+      if (w < 3) load_words(sm.side.win[buf] + 64 * w, wrs, e + 64 * w, l);
+      if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, l);
     }
   };
   int count = n_tiles, first = 0;
@@ -686,7 +702,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   if (count > 0) fetch(0, tile_at(0));
   bf16x8 qf[8], gf[8];
   f32x16 dq[4], pk[4];
-  const int row = q0 + w * 32 + r;
+  int row = q0 + w * 32 + r;
   load_row(qf, p.q + qoff, row, row < p.n_q, g);
   load_row(gf, p.dout + qoff, row, row < p.n_q, g);
   float nl = neg_inf(), nd = 0.f;
@@ -722,7 +738,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       }
       if (visit)
         dq_block<MODE, decltype(tail)::value>(sm, buf, b, row_at, col_at, qf, gf, dq, pk, nl, nd, p.c,
-                                              lane, p.n_k - (n_tiles - 1) * kTile - 32 * b,
+                                              p.n_k - (n_tiles - 1) * kTile - 32 * b,
                                               run, b == 0 ? tile.flat[0] : tile.flat[1], win, delta,
                                               rest);
     }
@@ -731,13 +747,15 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   visit_blocks(std::false_type{}, 0, ragged ? 2 * count - 2 : 2 * count);
   if (ragged) visit_blocks(std::true_type{}, 2 * count - 2, 2 * count);
   const float exact = half_sum(delta + rest), off_by = exact + nd;
+  const int l = lane_now(), half = l >> 5;
+  row = q0 + w * 32 + (l & 31);
   if (x >= p.dq_split.full) {
     if (row < p.n_q) {
       const int slot = x - p.dq_split.full;
       const size_t part = ((size_t)slot * part_rows(p.n_q) + (row - q0)) * kD;
-      store_part(p.part_a + part, dq, g);
-      store_part(p.part_b + part, pk, g);
-      if (g == 0) p.part_delta[(size_t)slot * 128 + (row - q0)] = exact;
+      store_part(p.part_a + part, dq, half);
+      store_part(p.part_b + part, pk, half);
+      if (half == 0) p.part_delta[(size_t)slot * 128 + (row - q0)] = exact;
     }
     return;
   }
@@ -746,8 +764,8 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
 #pragma unroll
     for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-off_by, pk[db][v], dq[db][v]);
   if (row < p.n_q) {
-    store_row(p.dq + qoff, row, dq, p.scale, g);
-    if (g == 0) p.neg_delta[(size_t)bh * p.n_rows + row] = -exact;
+    store_row(p.dq + qoff, row, dq, p.scale, half);
+    if (half == 0) p.neg_delta[(size_t)bh * p.n_rows + row] = -exact;
   }
 }
 

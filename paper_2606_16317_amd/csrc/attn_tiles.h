@@ -46,6 +46,14 @@ __device__ __forceinline__ float half_sum(float x) {
   return __builtin_bit_cast(float, (uint32_t)sw[0]) + __builtin_bit_cast(float, (uint32_t)sw[1]);
 }
 
+// This lane's number, taken anew: what rare paths derive from it then holds no register of a loop
+// around them, which the compiler otherwise computes it ahead of.
+__device__ __forceinline__ int lane_now() {
+  int x;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+  return x;
+}
+
 __device__ __forceinline__ int tile_swz(int row) { return ((row & 3) << 2) | ((row >> 2) & 3); }
 
 // LDS byte address of p.
