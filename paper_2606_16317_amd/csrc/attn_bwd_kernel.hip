@@ -775,6 +775,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
 __device__ __forceinline__ f32x4 sum_parts(const float* part, const WorkSplit& split, int slot0,
                                            int rows, int row, int col) {
   f32x4 x = f32x4{};
+#pragma unroll 8   // loads in flight; they come first, the sums keep their order
   for (int j = 0; j < split.parts; ++j)
     x += *reinterpret_cast<const f32x4*>(
         part + ((size_t)(slot0 + j * split.shared()) * rows + row) * kD + col);
@@ -790,6 +791,7 @@ __global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias
   const int row = at.group * 128 + local;
   if (row >= p.n_q) return;
   float exact = 0.f;
+#pragma unroll 8
   for (int j = 0; j < p.dq_split.parts; ++j)
     exact += p.part_delta[(size_t)(slot0 + j * p.dq_split.shared()) * 128 + local];
   float* nd = p.neg_delta + (size_t)at.bh * p.n_rows + row;

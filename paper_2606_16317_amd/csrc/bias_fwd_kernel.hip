@@ -286,10 +286,12 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
   const auto slot = [&](int i) { return (size_t)(slot0 + i * p.split.shared()); };
   const auto ml = [&](int i) { return p.part_ml + 2 * (128 * slot(i) + local); };
   float m = neg_inf();
+#pragma unroll 8
   for (int i = 0; i < p.split.parts; ++i) m = fmaxf(m, ml(i)[0]);
   float l = 0.f;
   f32x4 x = f32x4{};
   if (m > neg_inf())
+#pragma unroll 4
     for (int i = 0; i < p.split.parts; ++i) {
       const float f = exp2_fast(ml(i)[0] - m);
       l = fmaf(f, ml(i)[1], l);
