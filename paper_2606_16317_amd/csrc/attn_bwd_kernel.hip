@@ -25,32 +25,6 @@ namespace {
 
 constexpr int kMaxTiles = 4096;   // 64-row tiles that a visit list can hold
 
-// ---- per-row quantities ----------------------------------------------------------------
-
-// One row per 16 lanes: -lse * log2 e and -(dO . O), padded rows as rows that saw no key.
-__global__ __launch_bounds__(256) void bwd_rows_kernel(BwdParams p) {
-  const int row = blockIdx.x * 16 + (threadIdx.x >> 4);
-  const int bh = blockIdx.y;
-  const int part = threadIdx.x & 15;
-  if (row >= p.n_rows) return;
-  float dot = 0.f, nl = neg_inf();
-  if (row < p.n_q) {
-    const size_t at = ((size_t)bh * p.n_q + row) * kD + part * 8;
-    const bf16x8 a = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p.o + at));
-    const bf16x8 b = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4*>(p.dout + at));
-#pragma unroll
-    for (int i = 0; i < 8; ++i) dot = fmaf((float)a[i], (float)b[i], dot);
-#pragma unroll
-    for (int m = 8; m >= 1; m >>= 1) dot += __shfl_xor(dot, m);
-    const float l = p.lse[(size_t)bh * p.n_q + row];
-    if (l > neg_inf()) nl = -l * 1.4426950408889634f;
-  }
-  if (part == 0) {
-    p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
-    p.neg_delta[(size_t)bh * p.n_rows + row] = -dot;
-  }
-}
-
 // ---- visit lists -------------------------------------------------------------------------
 
 // What a workgroup visits, in order: tiles of the streamed axis that have an open pair, and for
@@ -705,10 +679,24 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   int row = q0 + w * 32 + r;
   load_row(qf, p.q + qoff, row, row < p.n_q, g);
   load_row(gf, p.dout + qoff, row, row < p.n_q, g);
+  // -lse * log2 e and -(dO . O); for the dk, dv kernel padded rows are rows that saw no key
   float nl = neg_inf(), nd = 0.f;
-  if (row < p.n_q) {
-    nl = p.neg_lse2[(size_t)bh * p.n_rows + row];
-    nd = p.neg_delta[(size_t)bh * p.n_rows + row];
+  {
+    bf16x8 of[8];
+    load_row(of, p.o + qoff, row, row < p.n_q, g);
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) nd = fmaf(-(float)of[i][j], (float)gf[i][j], nd);
+    nd = half_sum(nd);
+    if (row < p.n_q) {
+      const float l = p.lse[(size_t)bh * p.n_q + row];
+      if (l > neg_inf()) nl = -l * 1.4426950408889634f;
+    }
+    if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
+      p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
+      p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // of a row that is joined or not there
+    }
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
@@ -875,7 +863,6 @@ hipError_t launch_mode(const BwdParams& p, hipStream_t stream) {
     if (e != hipSuccess) return e;
   }
   if (p.bh > 0 && p.n_q > 0) {
-    hipLaunchKernelGGL(bwd_rows_kernel, dim3((p.n_rows + 15) / 16, p.bh), dim3(256), 0, stream, p);
     hipLaunchKernelGGL((bwd_dq_kernel<MODE>), dim3(p.dq_split.grid()), block, 0, stream, p);
     if (p.dq_split.shared() > 0)
       hipLaunchKernelGGL(bwd_join_dq_kernel, joined(p.dq_split, p.n_q), dim3(256), 0, stream, p, bias);
