@@ -370,10 +370,11 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
  *
  * over n_q queries and n_k keys, which need not be equally many.  bucket is a device int32
  * [n_q + n_k - 1] array over all values of j - i, from -(n_q - 1) up, shared by all heads;
- * table a device float [n_buckets][H].  A bucket outside [0, n_buckets), and a bias of -inf or
- * below -1e30, closes its pairs: they take no part (with such buckets for later keys the
- * attention is causal, for far ones it has a window).  A row with no open key gets zeros and an
- * LSE of -inf.
+ * table a device float [n_buckets][H].  A bucket outside [0, n_buckets), and a bias below -30000
+ * (-inf, the type's lowest value, and other masking numbers), closes its pairs: they take no part
+ * (with such buckets for later keys the attention is causal, for far ones it has a window).  Other
+ * biases are at most 30000.  A row with no open key gets zeros and an LSE of -inf.  q, k and v must
+ * be finite, at closed pairs too.
  *
  * q and o are contiguous bf16 [B][H][n_q][d]; k and v are bf16 [B][H][k_rows][d] of which the
  * first n_k <= k_rows rows of every head are keys (a cache with room; k_rows = n_k otherwise; the
@@ -387,7 +388,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
  *   dtable[i][h] = sum over b and the pairs of bucket i of dS          (float [n_buckets][H])
  *
  * whose sums are kept in 32 bits up to the parts of 128 keys and joined in 64, in a fixed order.
- * q, k, v and dout must be finite.
+ * dout must be finite too.
  *
  * Memory, alignment, overlap, workspace and device rules are those of dsattn_attn_bwd; table,
  * bucket, lse_out / lse and dtable are 4-byte aligned.

@@ -679,7 +679,7 @@ def dsattn_bias_attn_fwd(q, k, v, table, bucket, n_k=None, o=None, scale=None, l
                          workspace=None, stream=None):
     """Attention with a learned relative position bias: ``table`` (float32 [n_buckets, H]) holds
     a bias per bucket and head, ``bucket`` (int32 [n_q + n_k - 1]) the bucket of every j - i from
-    -(n_q - 1) up (outside [0, n_buckets): closed).  q is [B, H, n_q, 128]; k and v are [B, H,
+    -(n_q - 1) up (outside [0, n_buckets): closed, as are biases below -30000).  q is [B, H, n_q, 128]; k and v are [B, H,
     rows, 128], of which the first ``n_k`` (all by default) are keys.  Returns o; ``lse_out``
     (float32, B*H*n_q elements) receives the log-sum-exp.  ``workspace`` (a uint8 GPU tensor of
     ``dsattn_bias_attn_workspace_bytes``) is allocated here when not given."""

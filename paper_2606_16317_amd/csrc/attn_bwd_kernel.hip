@@ -693,6 +693,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       const float l = p.lse[(size_t)bh * p.n_q + row];
       if (l > neg_inf()) nl = -l * 1.4426950408889634f;
     }
+    if (nl == neg_inf()) nd = 0.f;   // whatever o and dO hold where there is no key
     if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
       p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
       p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // of a row that is joined or not there
@@ -815,7 +816,7 @@ __global__ __launch_bounds__(256) void bias_prepare_kernel(BiasParams b, int H, 
   if ((uint32_t)at >= (uint32_t)b.n_buckets) at = kRunClosed;
   if (there) {
     const float x = at < 0 ? neg_inf() : b.table[(size_t)at * H + h];
-    b.by_dist[(size_t)h * b.dist_stride + e] = x < -1e30f ? neg_inf() : x / scale;
+    b.by_dist[(size_t)h * b.dist_stride + e] = x < kClosedBelow ? neg_inf() : x / scale;
   }
   if (h == 0) {
     // the runs of this half wave: where neighbours differ

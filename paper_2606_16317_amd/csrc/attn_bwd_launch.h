@@ -34,6 +34,10 @@ constexpr bool is_step(int run) { return run >= kRunStep; }
 constexpr int run_first(int run) { return is_step(run) ? (run >> 10 & 1023) - 1 : run; }
 constexpr int run_last(int run) { return is_step(run) ? (run & 1023) - 1 : run; }
 constexpr int run_pos(int run) { return run >> 20 & 1023; }
+// Biases below this close their pairs.  Next to any other key exp of them is zero; in a row of
+// nothing else they would be open, but with logits and an LSE of that size in 32 bits, one step of
+// which (2^-9 here) goes into the recomputed probabilities as a factor.
+constexpr float kClosedBelow = -30000.f;
 constexpr int kMaxBuckets = 512;   // what the backward pass keeps of them in LDS
 
 // Fill by_dist and runs.

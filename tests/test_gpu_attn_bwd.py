@@ -114,6 +114,44 @@ def test_mask_that_keeps_nothing_and_mask_that_keeps_all():
     assert all(torch.equal(a[n], b[n]) for n in a)
 
 
+@pytest.mark.parametrize("H,N", [(128, 500), (130, 500), (515, 100), (700, 70)])
+def test_whole_rounds_of_workgroups_and_a_remainder(H, N):
+    """512 row groups at a time go without a split, the rest may be shared: none, few or most."""
+    from _grad_ref import Ref, random_qkv, skip_pairs
+
+    announce(f"backward H={H} N={N}")
+    q, k, v, do = random_qkv(1, H, N, N, H)
+    ref = Ref(q, k, v, do)
+    print(ref.check(**backward(q, k, v, ref, do)), flush=True)
+    mask = random_mask(1, H, N, 32, 32, 0.5, 6)
+    ref = Ref(q, k, v, do, skip=skip_pairs(mask, N, 32, 32))
+    got = backward(q, k, v, ref, do, mask_in=mask, tile_q=32, tile_k=32)
+    print(ref.check(**got), flush=True)
+
+
+def test_masked_places_may_hold_anything():
+    """NaN and infinities in rows that kept nothing, and in keys that no row kept, go nowhere."""
+    import paper_2606_16317_amd as dsa
+    from _grad_ref import Ref, random_qkv, skip_pairs
+
+    announce("NaN in masked places")
+    N, tile = 400, 32
+    q, k, v, do = random_qkv(1, 2, N, N, 14)
+    mask = random_mask(1, 2, N, tile, tile, 0.5, 4)
+    mask[:, :, 3] = mask[:, :, 12] = 1           # rows, the ragged last ones among them
+    mask[..., 5] = mask[..., 12] = 1             # keys
+    ref = Ref(q, k, v, do, skip=skip_pairs(mask, N, tile, tile))
+    o = ref.o.to(torch.bfloat16)
+    for lo, hi in ((96, 128), (384, 400)):
+        for x, bad in ((q, math.nan), (do, math.inf), (o, math.nan)):
+            x[:, :, lo:hi] = bad
+    for lo, hi in ((160, 192), (384, 400)):
+        k[:, :, lo:hi], v[:, :, lo:hi] = math.nan, -math.inf
+    got = dsa.dsattn_attn_bwd(dsa.RULE_MASK, q, k, v, o, ref.lse.float(), do, mask_in=mask,
+                              tile_q=tile, tile_k=tile)
+    print(ref.check(dq=got[0], dk=got[1], dv=got[2]), flush=True)
+
+
 @pytest.mark.parametrize("rule,param,tile_q,tile_k", [
     ("RULE_DENSE", 0.0, 128, 64), ("RULE_DYNSPARSE_LAMBDA", -3.0, 128, 64),
     ("RULE_DYNSPARSE_LAMBDA", -3.0, 32, 32), ("RULE_DYNSPARSE_LAMBDA", -3.0, 32, 128),

@@ -126,7 +126,7 @@ def test_longer_rows_and_more_workgroups():
 
 
 def test_closed_by_the_table():
-    """A bias of -inf, or below -1e30, closes a bucket for its head alone; a row may keep none."""
+    """A bias of -inf, or below -30000, closes a bucket for its head alone; a row may keep none."""
     from _grad_ref import Ref, distance_matrix, random_qkv
 
     announce("closed by the table")
@@ -145,6 +145,76 @@ def test_closed_by_the_table():
     assert torch.isinf(ref.lse).sum() == 1
     print(ref.check(**forward(q, k, v, table, m)), flush=True)
     print(ref.check(**backward(q, k, v, table, m, ref, do)), flush=True)
+
+
+@pytest.mark.parametrize("low", [-math.inf, -3.4e38, -1e9, -65504.0, -3.1e4, -2.9e4, -1e4])
+def test_masking_numbers(low):
+    """Masking numbers close their pairs, and leave rows with nothing else without a key; down to
+    -30000 they are biases, which rows with nothing else share."""
+    from _grad_ref import Ref, distance_matrix, random_qkv
+
+    announce(f"masking number {low}")
+    n = 200
+    q, k, v, do = random_qkv(1, 2, n, n, 3)
+    d = torch.arange(-(n - 1), n)
+    m = torch.where(d > 40, 0, 1).to(torch.int32).cuda()      # later keys far enough have a value
+    table = torch.tensor([[0.25, -0.5], [low, low]]).cuda()
+    at = distance_matrix(m, n, n)
+    bias = table.double().t()[:, at.long()]
+    if low < -3e4:
+        bias = bias.masked_fill(bias < -3e4, -math.inf)
+    ref = Ref(q, k, v, do, bias=bias)
+    ref.add_table(at, 2)
+    assert torch.isinf(ref.lse).any() == (low < -3e4)
+    print(ref.check(**forward(q, k, v, table, m)), flush=True)
+    print(ref.check(**backward(q, k, v, table, m, ref, do)), flush=True)
+
+
+@pytest.mark.parametrize("H,n_q,n_k", [(128, 500, 500), (130, 500, 300), (515, 100, 200),
+                                       (700, 1, 300)])
+@pytest.mark.parametrize("kind", ["both", "random"])
+def test_whole_rounds_of_workgroups_and_a_remainder(H, n_q, n_k, kind):
+    """512 row groups at a time go without a split, the rest may be shared: none, few or most."""
+    announce(f"bias step H={H} n_q={n_q} n_k={n_k} {kind}")
+    q, k, v, do, table, m, ref = make(1, H, n_q, n_k, kind, H)
+    print(ref.check(**forward(q, k, v, table, m)), flush=True)
+    print(ref.check(**backward(q, k, v, table, m, ref, do)), flush=True)
+
+
+def test_cache_beyond_32_bit_offsets():
+    """A token over 40 heads of 450000 rows each, 2.3e9 numbers, of which 700 are keys."""
+    import paper_2606_16317_amd as dsa
+
+    announce("cache of 2.3e9 numbers")
+    H, rows, n = 40, 450000, 700
+    q, k, v, _, table, m, ref = make(1, H, 1, n, "causal", 77)
+    cache = [torch.empty(1, H, rows, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    for c, x in zip(cache, (k, v)):
+        c[:, :, :n] = x
+    lse = torch.empty(1, H, 1, device="cuda")
+    o = dsa.dsattn_bias_attn_fwd(q, *cache, table, m, n_k=n, lse_out=lse)
+    print(ref.check(o=o, lse=lse), flush=True)
+
+
+def test_gradients_beyond_32_bit_offsets():
+    """65 heads of 262144 keys, 2.2e9 numbers; the last head against 64 bits."""
+    import paper_2606_16317_amd as dsa
+    from _grad_ref import Ref, distance_matrix, random_qkv
+
+    announce("gradients of 2.2e9 numbers")
+    H, n_q, n_k = 65, 33, 262144
+    m, nb = bucket_map("both", n_q, n_k, 0)
+    table = torch.randn(nb, H, generator=torch.Generator().manual_seed(2)).cuda()
+    q, k, v, do = random_qkv(1, 1, n_q, n_k, 8)
+    at = distance_matrix(m, n_q, n_k)
+    ref = Ref(q, k, v, do, bias=table[:, -1:].double().t()[:, at.long()])
+    ref.add_table(at, nb)
+    full = lambda x: torch.cat([x.new_zeros(1, H - 1, *x.shape[2:]), x], 1)
+    lse = ref.lse.float()
+    got = dsa.dsattn_bias_attn_bwd(*(full(x) for x in (q, k, v)), table, m,
+                                   full(ref.o.to(torch.bfloat16)), full(lse), full(do))
+    got = dict(zip(("dq", "dk", "dv"), (x[:, -1:] for x in got[:3])), dtable=got[3][:, -1:])
+    print(ref.check(**got), flush=True)
 
 
 @pytest.mark.parametrize("n_q,n_k", [(3, 0), (0, 3), (0, 0)])
