@@ -315,6 +315,7 @@ __device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uin
 #pragma unroll
   for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
   sched_fence();
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
     if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
@@ -343,6 +344,7 @@ __device__ __forceinline__ void dkv_block(DkvSmem<MODE>& sm, int buf, int b, uin
     }
     sched_fence();
   }
+  __builtin_amdgcn_s_setprio(0);
   // of a mixed block its sums by distance instead, of one with a step the parts above and below it
   if constexpr (MODE == kBwdBias) {
     if (is_step(bias.run)) {
@@ -415,7 +417,8 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = blockIdx.x;
-  const Place at = place_of(MODE == kBwdBias, p.dkv_split.unit(x), p.bh, (p.n_k + 127) / 128, false);
+  const Place at = place_of(p.dkv_split, MODE == kBwdBias, p.dkv_split.unit(x), p.bh,
+                            (p.n_k + 127) / 128, false);
   const int bh = at.bh, key0 = at.group * 128;
   const int n_tiles = (p.n_q + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
@@ -593,6 +596,7 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
 #pragma unroll
   for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
   sched_fence();
+  __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
     if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
@@ -620,6 +624,7 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
     }
     sched_fence();
   }
+  __builtin_amdgcn_s_setprio(0);
   // a sum of up to 2^18 block sums: what each addition rounds off is kept beside it
   const float x = delta + sum, y = x - delta;
   rest += (delta - (x - y)) + (sum - y);
@@ -632,7 +637,8 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = blockIdx.x;
-  const Place at = place_of(MODE == kBwdBias, p.dq_split.unit(x), p.bh, (p.n_q + 127) / 128, true);
+  const Place at = place_of(p.dq_split, MODE == kBwdBias, p.dq_split.unit(x), p.bh,
+                            (p.n_q + 127) / 128, true);
   const int bh = at.bh, q0 = at.group * 128;
   const int n_tiles = (p.n_k + kTile - 1) / kTile;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.n_k * kD;
@@ -776,7 +782,7 @@ __global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias
   const int rows = part_rows(p.n_q), col = 4 * (threadIdx.x & 31);
   const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
   if (slot0 >= p.dq_split.shared()) return;
-  const Place at = place_of(bias, p.dq_split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
+  const Place at = place_of(p.dq_split, bias, p.dq_split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
   const int row = at.group * 128 + local;
   if (row >= p.n_q) return;
   float exact = 0.f;
@@ -798,7 +804,7 @@ __global__ __launch_bounds__(256) void bwd_join_dkv_kernel(BwdParams p, bool bia
   const int rows = part_rows(p.n_k), col = 4 * (threadIdx.x & 31);
   const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
   if (slot0 >= p.dkv_split.shared()) return;
-  const Place at = place_of(bias, p.dkv_split.full + slot0, p.bh, (p.n_k + 127) / 128, false);
+  const Place at = place_of(p.dkv_split, bias, p.dkv_split.full + slot0, p.bh, (p.n_k + 127) / 128, false);
   const int row = at.group * 128 + local;
   if (row >= p.n_k) return;
   const size_t out = ((size_t)at.bh * p.n_k + row) * kD + col;
@@ -840,10 +846,11 @@ __global__ __launch_bounds__(1024) void bias_dtable_kernel(BwdParams p, int B, i
   double x = 0.0;
   if (i < n)
     for (int j = w; j < B * groups; j += 16) {
-      const int unit = j / B * p.bh + j % B * p.H + h;   // see place_of
+      const int group = j / B, head = j % B * p.H + h;
+      const int unit = split.order == kGroupByGroup ? group * p.bh + head : head * groups + group;
       const int parts = unit < split.full ? 1 : split.parts;
       for (int k = 0; k < parts; ++k)
-        x += p.dtable_part[(size_t)(unit + k * split.shared()) * n + i];
+        x += p.dtable_part[(size_t)(split.workgroup(unit) + k * split.shared()) * n + i];
     }
   sum[w][lane] = x;
   __syncthreads();
@@ -884,9 +891,10 @@ hipError_t launch_mode(const BwdParams& p, hipStream_t stream) {
 int bwd_padded_rows(int n_q) { return (n_q + kTile - 1) / kTile * kTile; }
 
 // A part's 128 KiB of sums are written and read at about 4.5 TB/s, 0.06 us; a tile takes 3.5 us.
-WorkSplit bwd_split(int bh, int n_own, int n_streamed) {
-    return make_split((long long)bh * ((n_own + 127) / 128), (n_streamed + kTile - 1) / kTile,
-                    0.017 * part_rows(n_own) / 128);
+WorkSplit bwd_split(int mode, int bh, int n_own, int n_streamed) {
+  const long long units = (long long)bh * ((n_own + 127) / 128);
+  return make_split(units, (n_streamed + kTile - 1) / kTile, 0.017 * part_rows(n_own) / 128,
+                    unit_order(mode == kBwdBias, mode == kBwdMask, bh, units));
 }
 
 hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream) {

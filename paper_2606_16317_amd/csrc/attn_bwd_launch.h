@@ -79,7 +79,7 @@ struct BwdParams {
 int bwd_padded_rows(int n_q);
 
 // The launches' units.
-WorkSplit bwd_split(int bh, int n_own, int n_streamed);
+WorkSplit bwd_split(int mode, int bh, int n_own, int n_streamed);
 
 hipError_t launch_attn_bwd(int mode, const BwdParams& p, hipStream_t stream);
 

@@ -14,12 +14,27 @@ namespace dsattn {
 //
 // Two workgroups run on each of the 256 CUs at a time, 512 in all, so what is left over after
 // whole rounds of 512 units (all of a small problem) is cut into parts.
+enum UnitOrder { kGroupByGroup, kHeadByHead, kHeadsToXcds };
 struct WorkSplit {
   int units, full, parts;
+  UnitOrder order;
   __host__ __device__ int shared() const { return units - full; }
   __host__ __device__ int grid() const { return full + shared() * parts; }
   __host__ __device__ int slots() const { return shared() * parts; }
-  __device__ int unit(int x) const { return x < full ? x : full + (x - full) % shared(); }
+  // Workgroups go to the 8 XCDs in turn.  kHeadsToXcds: each gets a contiguous share of the units.
+  __device__ int unit(int x) const {
+    if (x >= full) return full + (x - full) % shared();
+    if (order != kHeadsToXcds) return x;
+    const int xcd = x & 7;
+    return xcd * (full >> 3) + min(xcd, full & 7) + (x >> 3);
+  }
+  // The workgroup that has a unit, or its first part.
+  __device__ int workgroup(int unit) const {
+    if (unit >= full || order != kHeadsToXcds) return unit;
+    const int most = full >> 3, more = full & 7, longer = more * (most + 1);
+    const int xcd = unit < longer ? unit / (most + 1) : more + (unit - longer) / most;
+    return 8 * (unit - xcd * most - min(xcd, more)) + xcd;
+  }
   __device__ int part(int x) const { return x < full ? 0 : (x - full) / shared(); }
   // This workgroup's share [first, last) of `count` visits.
   __device__ void share(int x, int count, int& first, int& last) const {
@@ -32,23 +47,34 @@ struct WorkSplit {
   }
 };
 
-// Head and 128-row group of a unit.  A bias that closes later keys leaves the first key group
-// and the last query group the most to do: with a bias these come first for all heads, so that no
-// long one starts late.  (Otherwise a head's groups stand together, whose tiles L2 then shares.)
+// Head and 128-row group of a unit: head after head, or group after group of all heads.  A bias that
+// closes later keys leaves the first key group and the last query group the most to do, so these
+// come first (queries: the own rows are queries, taken from behind).
 struct Place {
   int bh, group;
 };
-__device__ inline Place place_of(bool bias, int unit, int bh, int groups, bool queries) {
-  if (!bias) return Place{unit / groups, unit % groups};
-  const int group = unit / bh;
-  return Place{unit % bh, queries ? groups - 1 - group : group};
+__device__ inline Place place_of(const WorkSplit& split, bool bias, int unit, int bh, int groups,
+                                 bool queries) {
+  const bool by_group = split.order == kGroupByGroup;
+  const int group = by_group ? unit / bh : unit % groups;
+  return Place{by_group ? unit % bh : unit / groups, bias && queries ? groups - 1 - group : group};
+}
+
+// Workgroups that run on an XCD at a time stream the same head through its L2 where each XCD has a
+// share of heads (24 heads of 27280 rows forward with a bias 9.14 ms instead of 9.45, 10 of 32760
+// backward 18.78 instead of 18.84), which needs equal shares: not under a mask, whose heads keep
+// more or less, nor where a causal bias leaves a part of a head more than another (5 heads of 32760
+// backward 6.87 ms instead of 5.39, group by group).  Few rounds want the groups in order, too.
+inline UnitOrder unit_order(bool bias, bool mask, int bh, long long units) {
+  if (mask) return kHeadByHead;
+  return !bias || (bh % 8 == 0 && units >= 4 * 512) ? kHeadsToXcds : kGroupByGroup;
 }
 
 // Rows of a unit's partial sums.
 __host__ __device__ inline int part_rows(int n) { return n < 128 ? n : 128; }
 
 // tiles: what a unit streams, at most.  join: what a part adds to the join, in times of a tile.
-inline WorkSplit make_split(long long units, int tiles, double join) {
+inline WorkSplit make_split(long long units, int tiles, double join, UnitOrder order) {
   const int rest = (int)(units % 512);
   // Up to 256 workgroups have a CU each and take 0.6 of the time of two on one; a part begins
   // with about two tiles' time without products, and the join is a launch.
@@ -61,7 +87,7 @@ inline WorkSplit make_split(long long units, int tiles, double join) {
   if (rest > 0)
     for (int s = 2; s <= std::min(tiles / 2, 1024 / rest); ++s)
       if (cost(s) < cost(parts)) parts = s;
-  return WorkSplit{(int)units, parts == 1 ? (int)units : (int)units - rest, parts};
+  return WorkSplit{(int)units, parts == 1 ? (int)units : (int)units - rest, parts, order};
 }
 
 }  // namespace dsattn

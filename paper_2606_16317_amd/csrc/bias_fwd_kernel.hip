@@ -78,7 +78,7 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
   const int tid = threadIdx.x, lane = tid & 63, r = lane & 31, g = lane >> 5;
   const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int x = blockIdx.x;
-  const Place at = place_of(true, p.split.unit(x), p.bh, (p.n_q + 127) / 128, true);
+  const Place at = place_of(p.split, true, p.split.unit(x), p.bh, (p.n_q + 127) / 128, true);
   const int bh = at.bh, q0 = at.group * 128;
   const size_t qoff = (size_t)bh * p.n_q * kD, koff = (size_t)bh * p.k_rows * kD;
   const auto krs = row_buffer(p.k + koff, p.n_k), vrs = row_buffer(p.v + koff, p.n_k);
@@ -215,7 +215,6 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       bf16x8 a[RK];
 #pragma unroll
       for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
-      float mb[2] = {neg_inf(), neg_inf()};
       sched_fence();
 #pragma unroll
       for (int i = 0; i < 32; ++i) {
@@ -233,12 +232,6 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
           prob(2 * i + 1);
         } else if (i < 24) {
           prob(i + 8);
-        } else {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            const int j = 4 * (i - 24) + e;
-            mb[j >> 4] = maximum(mb[j >> 4], sn[j >> 4][j & 15]);
-          }
         }
         sched_fence();
       }
@@ -247,12 +240,9 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       for (int e = 0; e < 32; ++e) sum += xs[e];
       rs.l_half += sum;
       const int left = p.n_k - (t + 1) * kTile;
-      if (left < kTile) {   // the last tile is next: its maximum again, over the keys it has
-        mask_keys(sn, left - 4 * g);
-        mb[0] = block_max(sn[0]);
-        mb[1] = block_max(sn[1]);
-      }
-      m_hat = row_join(maximum(fmaf(mb[0], p.c, tb_next.flat[0]), fmaf(mb[1], p.c, tb_next.flat[1])));
+      if (left < kTile) mask_keys(sn, left - 4 * g);   // the last tile is next, and not full
+      m_hat = row_join(maximum(fmaf(block_max(sn[0]), p.c, tb_next.flat[0]),
+                               fmaf(block_max(sn[1]), p.c, tb_next.flat[1])));
       tb = tb_next;
       s[0] = sn[0];
       s[1] = sn[1];
@@ -280,7 +270,7 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
   const int rows = part_rows(p.n_q), col = 4 * (threadIdx.x & 31);
   const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
   if (slot0 >= p.split.shared()) return;
-  const Place at = place_of(true, p.split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
+  const Place at = place_of(p.split, true, p.split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
   const int row = at.group * 128 + local;
   if (row >= p.n_q) return;
   const auto slot = [&](int i) { return (size_t)(slot0 + i * p.split.shared()); };
@@ -309,8 +299,9 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
 
 // A part's 64 KiB are written and read at about 4.5 TB/s, 0.03 us; a tile takes 2 us.
 WorkSplit bias_fwd_split(int bh, int n_q, int n_k) {
-  return make_split((long long)bh * ((n_q + 127) / 128), (n_k + kTile - 1) / kTile,
-                    0.015 * part_rows(n_q) / 128);
+  const long long units = (long long)bh * ((n_q + 127) / 128);
+  return make_split(units, (n_k + kTile - 1) / kTile, 0.015 * part_rows(n_q) / 128,
+                    unit_order(true, false, bh, units));
 }
 
 hipError_t launch_bias_fwd(const BiasFwdParams& p, hipStream_t stream) {

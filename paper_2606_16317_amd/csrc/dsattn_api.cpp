@@ -794,34 +794,34 @@ size_t bwd_rows_bytes(int B, int H, int n) {
 }
 
 // Bytes of one of the two arrays of partial sums; the dq and the dk, dv kernel use them in turn.
-size_t bwd_part_bytes(int bh, int n_q, int n_k) {
+size_t bwd_part_bytes(int mode, int bh, int n_q, int n_k) {
   const auto floats = [](const dsattn::WorkSplit& s, int n) {
     return (size_t)s.slots() * (size_t)dsattn::part_rows(n) * kHeadDim;
   };
-  return round_up(std::max(floats(dsattn::bwd_split(bh, n_q, n_k), n_q),
-                           floats(dsattn::bwd_split(bh, n_k, n_q), n_k)) * sizeof(float));
+  return round_up(std::max(floats(dsattn::bwd_split(mode, bh, n_q, n_k), n_q),
+                           floats(dsattn::bwd_split(mode, bh, n_k, n_q), n_k)) * sizeof(float));
 }
 
-size_t bwd_delta_bytes(int bh, int n_q, int n_k) {
-  return round_up((size_t)dsattn::bwd_split(bh, n_q, n_k).slots() * 128 * sizeof(float));
+size_t bwd_delta_bytes(int mode, int bh, int n_q, int n_k) {
+  return round_up((size_t)dsattn::bwd_split(mode, bh, n_q, n_k).slots() * 128 * sizeof(float));
 }
 
-size_t bwd_bytes(int B, int H, int n_q, int n_k) {
-  return bwd_rows_bytes(B, H, n_q) + 2 * bwd_part_bytes(B * H, n_q, n_k) +
-         bwd_delta_bytes(B * H, n_q, n_k);
+size_t bwd_bytes(int mode, int B, int H, int n_q, int n_k) {
+  return bwd_rows_bytes(B, H, n_q) + 2 * bwd_part_bytes(mode, B * H, n_q, n_k) +
+         bwd_delta_bytes(mode, B * H, n_q, n_k);
 }
 
 // What both backward calls fill in alike, n_q and n_k set before.
-void bwd_slices(dsattn::BwdParams& p, Slices& ws) {
+void bwd_slices(int mode, dsattn::BwdParams& p, Slices& ws) {
   p.n_rows = dsattn::bwd_padded_rows(p.n_q);
   const size_t row_bytes = (size_t)p.bh * (size_t)p.n_rows * sizeof(float);
   p.neg_lse2 = static_cast<float*>(ws.take(row_bytes));
   p.neg_delta = static_cast<float*>(ws.take(row_bytes));
-  p.dq_split = dsattn::bwd_split(p.bh, p.n_q, p.n_k);
-  p.dkv_split = dsattn::bwd_split(p.bh, p.n_k, p.n_q);
-  p.part_a = static_cast<float*>(ws.take(bwd_part_bytes(p.bh, p.n_q, p.n_k)));
-  p.part_b = static_cast<float*>(ws.take(bwd_part_bytes(p.bh, p.n_q, p.n_k)));
-  p.part_delta = static_cast<float*>(ws.take(bwd_delta_bytes(p.bh, p.n_q, p.n_k)));
+  p.dq_split = dsattn::bwd_split(mode, p.bh, p.n_q, p.n_k);
+  p.dkv_split = dsattn::bwd_split(mode, p.bh, p.n_k, p.n_q);
+  p.part_a = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
+  p.part_b = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
+  p.part_delta = static_cast<float*>(ws.take(bwd_delta_bytes(mode, p.bh, p.n_q, p.n_k)));
 }
 
 bool sane_extents(int B, int H, int n) {
@@ -833,13 +833,14 @@ bool sane_extents(int B, int H, int n) {
 }  // namespace
 
 size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N) {
-  return sane_extents(B, H, N) ? bwd_bytes(B, H, N, N) : 0;
+  return sane_extents(B, H, N) ? bwd_bytes(dsattn::kBwdDense, B, H, N, N) : 0;
 }
 
 int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_size) {
   if (args == nullptr) return fail(DSATTN_EINVAL, "args must be non-null");
   const dsattn_bwd_args& a = *args;
   const bool masked = a.rule == DSATTN_RULE_MASK;
+  const int mode = masked ? dsattn::kBwdMask : dsattn::kBwdDense;
   if (a.rule == DSATTN_RULE_BLASST || a.rule == DSATTN_RULE_DYNSPARSE_RECALL ||
       a.rule == DSATTN_RULE_DYNSPARSE_LAMBDA)
     return fail(DSATTN_EUNSUPPORTED,
@@ -857,7 +858,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
     g_last_error.clear();
     return DSATTN_OK;
   }
-  const size_t need = bwd_bytes(a.B, a.H, a.N, a.N);
+  const size_t need = bwd_bytes(mode, a.B, a.H, a.N, a.N);
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t rows = (size_t)a.B * (size_t)a.H * (size_t)a.N, wide = rows * kHeadDim * 2;
   const int n_units = (a.N + a.tile_q - 1) / a.tile_q, n_dec = (a.N + a.tile_k - 1) / a.tile_k;
@@ -890,14 +891,13 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   p.c = (float)((double)a.scale * kLog2e);
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
-  bwd_slices(p, ws);
+  bwd_slices(mode, p, ws);
   p.mask = masked ? a.mask_in : nullptr;
   p.tile_q = a.tile_q;
   p.tile_k = a.tile_k;
   p.n_units = n_units;
   p.n_dec = n_dec;
-  const hipError_t e = dsattn::launch_attn_bwd(masked ? dsattn::kBwdMask : dsattn::kBwdDense, p,
-                                               a.stream);
+  const hipError_t e = dsattn::launch_attn_bwd(mode, p, a.stream);
   if (e != hipSuccess) return fail(DSATTN_ELAUNCH, "kernel launch failed: %s", hipGetErrorString(e));
   g_last_error.clear();
   return DSATTN_OK;
@@ -958,8 +958,8 @@ size_t bias_fwd_bytes(int B, int H, int n_q, int n_k) {
 }
 
 size_t bias_bwd_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
-  const size_t parts = (size_t)dsattn::bwd_split(B * H, n_k, n_q).grid();
-  return bias_layout_bytes(H, n_q, n_k) + bwd_bytes(B, H, n_q, n_k) +
+  const size_t parts = (size_t)dsattn::bwd_split(dsattn::kBwdBias, B * H, n_k, n_q).grid();
+  return bias_layout_bytes(H, n_q, n_k) + bwd_bytes(dsattn::kBwdBias, B, H, n_q, n_k) +
          round_up(parts * (size_t)n_buckets * sizeof(float));
 }
 
@@ -1082,7 +1082,7 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
   p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
-  bwd_slices(p, ws);
+  bwd_slices(dsattn::kBwdBias, p, ws);
   p.dtable = a.dtable;
   p.dtable_part = static_cast<float*>(
       ws.take((size_t)p.dkv_split.grid() * (size_t)a.n_buckets * sizeof(float)));

@@ -170,7 +170,7 @@ def test_masking_numbers(low):
     print(ref.check(**backward(q, k, v, table, m, ref, do)), flush=True)
 
 
-@pytest.mark.parametrize("H,n_q,n_k", [(128, 500, 500), (130, 500, 300), (515, 100, 200),
+@pytest.mark.parametrize("H,n_q,n_k", [(512, 70, 100), (171, 257, 120), (515, 100, 200),
                                        (700, 1, 300)])
 @pytest.mark.parametrize("kind", ["both", "random"])
 def test_whole_rounds_of_workgroups_and_a_remainder(H, n_q, n_k, kind):
