@@ -37,7 +37,6 @@ struct VisitList {
 };
 
 // Whether the 32 x 32 block of query block qb and key block kb has an open pair.
-template <int MODE>
 __device__ __forceinline__ bool block_open(const BwdParams& p, int bh, int qb, int kb) {
   if (32 * qb >= p.n_q || 32 * kb >= p.n_k) return false;
   const int u = 32 * qb / p.tile_q, d = 32 * kb / p.tile_k;
@@ -46,19 +45,26 @@ __device__ __forceinline__ bool block_open(const BwdParams& p, int bh, int qb, i
 
 // Fill the list: own 32-row blocks own0 .. own0 + 3, streamed tiles 0 .. n_tiles - 1.
 // Q_OWN: the own blocks are query blocks, the tiles key tiles.
-template <int MODE, bool Q_OWN>
+template <bool Q_OWN>
 __device__ __forceinline__ void build_list(VisitList& list, const BwdParams& p, int bh, int own0,
                                            int n_tiles) {
   const int tid = threadIdx.x, lane = tid & 63;
-  // every thread notes its tiles' bits in place, then the first wave closes the gaps in order
-  for (int t = tid; t < n_tiles; t += kThreads) {
-    uint32_t bits = 0;
-#pragma unroll 1
-    for (int j = 0; j < 8; ++j) {
-      const int b = 2 * t + (j >> 2), x = own0 + (j & 3);
-      if (Q_OWN ? block_open<MODE>(p, bh, x, b) : block_open<MODE>(p, bh, b, x)) bits |= 1u << j;
+  // eight threads a tile note its bits in place, four tiles at a time for their loads' sake, then
+  // the first wave closes the gaps in order
+  constexpr int kStep = kThreads / 8;
+  for (int t0 = tid >> 3; t0 < n_tiles; t0 += 4 * kStep) {
+    bool open[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = t0 + u * kStep, j = tid & 7, b = 2 * t + (j >> 2), x = own0 + (j & 3);
+      open[u] = t < n_tiles && (Q_OWN ? block_open(p, bh, x, b) : block_open(p, bh, b, x));
     }
-    list.bits[t] = (uint8_t)bits;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int t = t0 + u * kStep;
+      const uint32_t bits = (uint32_t)(__ballot(open[u]) >> (lane & 56)) & 0xffu;
+      if ((tid & 7) == 0 && t < n_tiles) list.bits[t] = (uint8_t)bits;
+    }
   }
   __syncthreads();
   if (tid < 64) {
@@ -80,35 +86,6 @@ __device__ __forceinline__ void build_list(VisitList& list, const BwdParams& p, 
 }
 
 // ---- position bias -----------------------------------------------------------------------
-
-// Distances key - query of a workgroup and a streamed tile: 128 + 64 - 1 of them, in windows of
-// kWindow words that begin with the tile's smallest.
-constexpr int kWindow = 192;
-
-// First and last streamed tile with an open run of distances (first > last: none).  e0(t) is the
-// smallest distance index of tile t.
-struct TileRange {
-  int first, last;
-};
-template <typename F>
-__device__ __forceinline__ void open_tiles(TileRange& range, const BiasParams& b, int n_tiles, F e0) {
-  if (threadIdx.x == 0) {
-    range.first = n_tiles;
-    range.last = -1;
-  }
-  __syncthreads();
-  for (int t = threadIdx.x; t < n_tiles; t += kThreads) {
-    const int e = e0(t);
-    const int j1 = min(b.n_runs - 1, (e + kWindow - 2) >> 5);
-    bool open = false;
-    for (int j = max(0, e >> 5); j <= j1; ++j) open |= b.runs[j] != kRunClosed;
-    if (open) {
-      atomicMin(&range.first, t);
-      atomicMax(&range.last, t);
-    }
-  }
-  __syncthreads();
-}
 
 // What a wave's two 32 x 32 blocks of a tile lie in, by ascending distance: run[j] as a word of
 // runs, but with the position counted from the tile's smallest distance, and the value at the
@@ -184,12 +161,12 @@ struct DkvBias {
   int32_t runs[2][64];
   float bins[kWaves][kMaxBuckets];         // sums over buckets
   float closed[32];                        // -inf, read by lanes whose key does not exist
-  TileRange range;
+  int ends[2];   // of the open runs, see open_tiles
 };
 struct DqBias {
   alignas(16) float win[2][kWindow];
   int32_t runs[2][64];
-  TileRange range;
+  int ends[2];   // of the open runs, see open_tiles
 };
 template <int MODE, typename BIAS>
 struct SideOf {
@@ -446,15 +423,21 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
     }
   };
 
+  bf16x8 kf[8], vf[8];
+  int key = key0 + w * 32 + r;
+  load_row(kf, p.k + koff, key, key < p.n_k, g);
+  load_row(vf, p.v + koff, key, key < p.n_k, g);
+
   int count = n_tiles, first = 0;
   if constexpr (MODE == kBwdMask) {
-    build_list<MODE, false>(sm.side, p, bh, key0 / 32, n_tiles);
+    build_list<false>(sm.side, p, bh, key0 / 32, n_tiles);
     count = sm.side.count;
   }
   if constexpr (MODE == kBwdBias) {
-    open_tiles(sm.side.range, p.bias, n_tiles, first_distance);
-    first = sm.side.range.first;
-    count = max(0, sm.side.range.last - first + 1);
+    const TileRange open = open_tiles<-1>(sm.side.ends, p.bias.runs, p.bias.n_runs, n_tiles,
+                                          first_distance(0));
+    first = open.first;
+    count = max(0, open.last - first + 1);
     for (int i = tid; i < kWaves * kMaxBuckets; i += kThreads) sm.side.bins[0][i] = 0.f;
     if (tid < 32) sm.side.closed[tid] = neg_inf();
     __syncthreads();
@@ -471,11 +454,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
   };
 
   if (count > 0) fetch(0, tile_at(0));
-  bf16x8 kf[8], vf[8];
   f32x16 dk[4], dv[4];
-  int key = key0 + w * 32 + r;
-  load_row(kf, p.k + koff, key, key < p.n_k, g);
-  load_row(vf, p.v + koff, key, key < p.n_k, g);
 #pragma unroll
   for (int db = 0; db < 4; ++db) dk[db] = dv[db] = f32x16{};
 
@@ -659,15 +638,23 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       if (w == 3) load_words(sm.side.runs[buf], rrs, e >> 5, l);
     }
   };
+  bf16x8 qf[8], gf[8], of[8];
+  int row = q0 + w * 32 + r;
+  load_row(qf, p.q + qoff, row, row < p.n_q, g);
+  load_row(gf, p.dout + qoff, row, row < p.n_q, g);
+  load_row(of, p.o + qoff, row, row < p.n_q, g);
+  const float lse = row < p.n_q ? p.lse[(size_t)bh * p.n_q + row] : neg_inf();
+
   int count = n_tiles, first = 0;
   if constexpr (MODE == kBwdMask) {
-    build_list<MODE, true>(sm.side, p, bh, q0 / 32, n_tiles);
+    build_list<true>(sm.side, p, bh, q0 / 32, n_tiles);
     count = sm.side.count;
   }
   if constexpr (MODE == kBwdBias) {
-    open_tiles(sm.side.range, p.bias, n_tiles, first_distance);
-    first = sm.side.range.first;
-    count = max(0, sm.side.range.last - first + 1);
+    const TileRange open = open_tiles<1>(sm.side.ends, p.bias.runs, p.bias.n_runs, n_tiles,
+                                         first_distance(0));
+    first = open.first;
+    count = max(0, open.last - first + 1);
   }
   int skip, end;
   p.dq_split.share(x, count, skip, end);
@@ -680,30 +667,21 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       return first + i;
   };
   if (count > 0) fetch(0, tile_at(0));
-  bf16x8 qf[8], gf[8];
   f32x16 dq[4], pk[4];
-  int row = q0 + w * 32 + r;
-  load_row(qf, p.q + qoff, row, row < p.n_q, g);
-  load_row(gf, p.dout + qoff, row, row < p.n_q, g);
   // -lse * log2 e and -(dO . O); for the dk, dv kernel padded rows are rows that saw no key
   float nl = neg_inf(), nd = 0.f;
-  {
-    bf16x8 of[8];
-    load_row(of, p.o + qoff, row, row < p.n_q, g);
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) nd = fmaf(-(float)of[i][j], (float)gf[i][j], nd);
-    nd = half_sum(nd);
-    if (row < p.n_q) {
-      const float l = p.lse[(size_t)bh * p.n_q + row];
-      if (l > neg_inf()) nl = -l * 1.4426950408889634f;
-    }
-    if (nl == neg_inf()) nd = 0.f;   // whatever o and dO hold where there is no key
-    if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
-      p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
-      p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // of a row that is joined or not there
-    }
+    for (int j = 0; j < 8; ++j) nd = fmaf(-(float)of[i][j], (float)gf[i][j], nd);
+  nd = half_sum(nd);
+  if (lse > neg_inf())
+    nl = -lse * 1.4426950408889634f;
+  else
+    nd = 0.f;   // whatever o and dO hold where there is no key
+  if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
+    p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
+    p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // of a row that is joined or not there
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};

@@ -71,7 +71,8 @@ __device__ __forceinline__ uint32_t scalar(uint32_t x) {
   asm volatile("" : "+s"(x));
   return x;
 }
-__device__ __forceinline__ void here(uint32_t& x) { asm volatile("" : "+v"(x)); }
+template <typename T>
+__device__ __forceinline__ void here(T& x) { asm volatile("" : "+v"(x)); }
 struct InLane {};
 __device__ __forceinline__ uint32_t flip(uint32_t at, uint32_t block, uint32_t x) {
   return at ^ scalar(block | x);
@@ -184,6 +185,49 @@ __device__ __forceinline__ void load_words(const void* dst, __amdgpu_buffer_rsrc
 // tiles read before can be overwritten.
 __device__ __forceinline__ void tiles_ready() {
   asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+}
+
+// Distances key - query of a workgroup's 128 rows and a streamed tile: 128 + 64 - 1 of them, in
+// windows of kWindow words that begin with the tile's smallest.
+constexpr int kWindow = 192;
+
+// First and last streamed tile with an open run of distances (first > last: none).  The window of
+// tile t begins at distance index e0 + DIR * kTile * t; `ends` is LDS for the first and the last open
+// run that any of them reaches into.
+struct TileRange {
+  int first, last;
+};
+template <int DIR>
+__device__ __forceinline__ TileRange open_tiles(int (&ends)[2], const int32_t* runs, int n_runs,
+                                                int n_tiles, int e0) {
+  static_assert(kTile == 64, "the shifts below");
+  if (threadIdx.x == 0) {
+    ends[0] = n_runs;
+    ends[1] = -1;
+  }
+  __syncthreads();
+  const int lane = threadIdx.x & 63, e1 = e0 + DIR * kTile * (n_tiles - 1);
+  const int j0 = max(0, min(e0, e1) >> 5), j1 = min(n_runs - 1, (max(e0, e1) + kWindow - 2) >> 5);
+  int first = n_runs, last = -1;
+  for (int j = j0 + (int)(threadIdx.x & ~63u); j <= j1; j += kThreads) {
+    const bool open = j + lane <= j1 && runs[min(j + lane, j1)] != -1;   // kRunClosed
+    const uint64_t have = __ballot(open);
+    if (have == 0) continue;
+    first = min(first, j + __ffsll((unsigned long long)have) - 1);
+    last = max(last, j + 63 - __clzll((long long)have));
+  }
+  if (lane == 0 && last >= 0) {
+    atomicMin(&ends[0], first);
+    atomicMax(&ends[1], last);
+  }
+  __syncthreads();
+  first = __builtin_amdgcn_readfirstlane(ends[0]);
+  last = __builtin_amdgcn_readfirstlane(ends[1]);
+  if (last < 0) return TileRange{n_tiles, -1};
+  // tile t reaches into run j where 32 j - (kWindow - 2) <= e0 + DIR * kTile * t <= 32 j + 31
+  const int t0 = DIR > 0 ? 32 * first - (kWindow - 2) - e0 : e0 - 32 * last - 31;
+  const int t1 = DIR > 0 ? 32 * last + 31 - e0 : e0 - 32 * first + (kWindow - 2);
+  return TileRange{max(0, (t0 + 63) >> 6), min(n_tiles - 1, t1 >> 6)};
 }
 
 // Own-row fragments (B operands, all eight k-steps) of one row of a head; zeros where !valid.

@@ -15,7 +15,6 @@
 namespace dsattn {
 namespace {
 
-constexpr int kWindow = 192;             // distances of 128 queries and 64 keys, and one
 constexpr float kRescaleSlack = 8.0f;    // log2 units
 
 struct FwdSmem {
@@ -23,7 +22,7 @@ struct FwdSmem {
   alignas(16) uint16_t v[2][kTileElems];
   alignas(16) float win[2][kWindow];
   int32_t runs[2][64];
-  int first, last;
+  int ends[2];
 };
 
 __device__ __forceinline__ float maximum(float a, float b) { return __builtin_elementwise_maximum(a, b); }
@@ -66,6 +65,7 @@ __device__ __forceinline__ float row_join(float x) {
 }
 
 __device__ __forceinline__ void mask_keys(f32x16 (&s)[2], int lim) {
+  here(lim);   // (or the compiler selects in every tile instead of branching in the last)
 #pragma unroll
   for (int b = 0; b < 2; ++b)
 #pragma unroll
@@ -88,25 +88,15 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
   const uint32_t row_at = lds_addr(sm.k) + row_lane(r, g), col_at = lds_addr(sm.v) + col_lane(lane);
   const auto first_distance = [&](int t) { return t * kTile - (q0 + 127) + p.n_q - 1; };
 
-  // tiles with an open run of distances, and of those this split's share
-  if (tid == 0) {
-    sm.first = 0x7fffffff;
-    sm.last = -1;
-  }
-  __syncthreads();
-  const int n_tiles = (p.n_k + kTile - 1) / kTile;
-  for (int t = tid; t < n_tiles; t += kThreads) {
-    const int e = first_distance(t), j1 = min(p.bias.n_runs - 1, (e + kWindow - 2) >> 5);
-    bool open = false;
-    for (int j = max(0, e >> 5); j <= j1; ++j) open |= p.bias.runs[j] != kRunClosed;
-    if (open) {
-      atomicMin(&sm.first, t);
-      atomicMax(&sm.last, t);
-    }
-  }
-  __syncthreads();
-  int t0 = __builtin_amdgcn_readfirstlane(sm.first);
-  int t1 = __builtin_amdgcn_readfirstlane(sm.last) + 1;   // none open: t1 = 0 < t0
+  const int row = q0 + 32 * w + r;
+  const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
+  bf16x8 qf[8];
+  load_row(qf, p.q + qoff, row, row < p.n_q, g);
+
+  // tiles with an open run of distances, and of those this workgroup's share
+  const TileRange open = open_tiles<1>(sm.ends, p.bias.runs, p.bias.n_runs,
+                                       (p.n_k + kTile - 1) / kTile, first_distance(0));
+  int t0 = open.first, t1 = open.last + 1;   // none open: t1 = 0 <= t0
   if (t0 < t1) {
     int first, last;
     p.split.share(x, t1 - t0, first, last);
@@ -122,8 +112,6 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
   };
   auto fetch_v = [&](int buf, int t) { load_tile(sm.v[buf], vrs, off, t * kTile, w); };
 
-  const int row = q0 + 32 * w + r;
-  const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
   f32x16 o[4];
 #pragma unroll
   for (int db = 0; db < 4; ++db) o[db] = f32x16{};
@@ -133,8 +121,6 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
     fetch_k(0, t0);
     fetch_v(0, t0);
     if (t0 + 1 < t1) fetch_k(1, t0 + 1);
-    bf16x8 qf[8];
-    load_row(qf, p.q + qoff, row, row < p.n_q, g);
     tiles_ready();
 
     // The bias of tile t in buffer buf: which blocks are mixed, and what the others add.
