@@ -497,17 +497,18 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dkv_kernel(BwdParams p) {
       if ((i & 63) == 63) far.flush(sm.side.bins[w]);
     }
   }
-  key = key0 + w * 32 + (lane_now() & 31);
-  if (key < p.n_k) {
-    const int g = lane_now() >> 5;
-    if (x < p.dkv_split.full) {
-      store_row(p.dv + koff, key, dv, 1.f, g);
-      store_row(p.dk + koff, key, dk, p.scale, g);
-    } else {
-      const size_t part = ((size_t)(x - p.dkv_split.full) * part_rows(p.n_k) + (key - key0)) * kD;
-      store_part(p.part_a + part, dk, g);
-      store_part(p.part_b + part, dv, g);
+  const int l = lane_now(), half = l >> 5;
+  key = key0 + w * 32 + (l & 31);
+  if (x < p.dkv_split.full) {
+    if (key < p.n_k) {
+      store_row(p.dv + koff, key, dv, 1.f, half);
+      store_row(p.dk + koff, key, dk, p.scale, half);
     }
+  } else if (own) {
+    const size_t slot = x - p.dkv_split.full;
+    const int rows = part_rows(p.n_k);
+    store_part(p.part_a + slot * rows * kD, dk, rows, w, l);
+    store_part(p.part_b + slot * rows * kD, dv, rows, w, l);
   }
   if constexpr (MODE == kBwdBias) {
     far.flush(sm.side.bins[w]);
@@ -681,7 +682,8 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     nd = 0.f;   // whatever o and dO hold where there is no key
   if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
     p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
-    p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // of a row that is joined or not there
+    p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // stays where there is no such row
+    if (x >= p.dq_split.full) p.part_prime[(size_t)(x - p.dq_split.full) * 128 + (row - q0)] = nd;
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
@@ -723,12 +725,12 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const int l = lane_now(), half = l >> 5;
   row = q0 + w * 32 + (l & 31);
   if (x >= p.dq_split.full) {
-    if (row < p.n_q) {
-      const int slot = x - p.dq_split.full;
-      const size_t part = ((size_t)slot * part_rows(p.n_q) + (row - q0)) * kD;
-      store_part(p.part_a + part, dq, half);
-      store_part(p.part_b + part, pk, half);
-      if (half == 0) p.part_delta[(size_t)slot * 128 + (row - q0)] = exact;
+    if (own) {
+      const size_t slot = x - p.dq_split.full;
+      const int rows = part_rows(p.n_q);
+      store_part(p.part_a + slot * rows * kD, dq, rows, w, l);
+      store_part(p.part_b + slot * rows * kD, pk, rows, w, l);
+      if (half == 0) p.part_delta[slot * 128 + (row - q0)] = exact;
     }
     return;
   }
@@ -744,50 +746,48 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
 
 // ---- joins -------------------------------------------------------------------------------
 
-// Sum of a shared unit's parts in their order, 4 columns of one row; slot0: the first part's slot.
-__device__ __forceinline__ f32x4 sum_parts(const float* part, const WorkSplit& split, int slot0,
-                                           int rows, int row, int col) {
+// Sum of a shared unit's parts in their order, four columns of one row.
+__device__ __forceinline__ f32x4 sum_parts(const float* part, const WorkSplit& split, int rows,
+                                           const PartPlace& me) {
   f32x4 x = f32x4{};
 #pragma unroll 8   // loads in flight; they come first, the sums keep their order
   for (int j = 0; j < split.parts; ++j)
     x += *reinterpret_cast<const f32x4*>(
-        part + ((size_t)(slot0 + j * split.shared()) * rows + row) * kD + col);
+        part + (size_t)(me.slot0 + j * split.shared()) * rows * kD + me.offset);
   return x;
 }
 
-// dq and delta, as at the end of bwd_dq_kernel.  32 lanes a row.
+// dq and delta, as at the end of bwd_dq_kernel.
 __global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias) {
-  const int rows = part_rows(p.n_q), col = 4 * (threadIdx.x & 31);
-  const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
-  if (slot0 >= p.dq_split.shared()) return;
-  const Place at = place_of(p.dq_split, bias, p.dq_split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
-  const int row = at.group * 128 + local;
+  const int rows = part_rows(p.n_q);
+  const PartPlace me = part_place(blockIdx.x * 256 + threadIdx.x, rows);
+  if (me.slot0 >= p.dq_split.shared()) return;
+  const Place at = place_of(p.dq_split, bias, p.dq_split.full + me.slot0, p.bh, (p.n_q + 127) / 128, true);
+  const int row = at.group * 128 + me.row;
   if (row >= p.n_q) return;
   float exact = 0.f;
 #pragma unroll 8
   for (int j = 0; j < p.dq_split.parts; ++j)
-    exact += p.part_delta[(size_t)(slot0 + j * p.dq_split.shared()) * 128 + local];
-  float* nd = p.neg_delta + (size_t)at.bh * p.n_rows + row;
-  const float off_by = exact + *nd;
-  f32x4 x = sum_parts(p.part_a, p.dq_split, slot0, rows, local, col);
-  const f32x4 y = sum_parts(p.part_b, p.dq_split, slot0, rows, local, col);
+    exact += p.part_delta[(size_t)(me.slot0 + j * p.dq_split.shared()) * 128 + me.row];
+  const float off_by = exact + p.part_prime[(size_t)me.slot0 * 128 + me.row];
+  f32x4 x = sum_parts(p.part_a, p.dq_split, rows, me);
+  const f32x4 y = sum_parts(p.part_b, p.dq_split, rows, me);
 #pragma unroll
   for (int t = 0; t < 4; ++t) x[t] = fmaf(-off_by, y[t], x[t]);
-  store_cols(p.dq + ((size_t)at.bh * p.n_q + row) * kD + col, x, p.scale);
-  __builtin_amdgcn_wave_barrier();   // the row's lanes, all of one wave, have read it
-  if (col == 0) *nd = -exact;
+  store_cols(p.dq + ((size_t)at.bh * p.n_q + row) * kD + me.col, x, p.scale);
+  if (me.col == 0) p.neg_delta[(size_t)at.bh * p.n_rows + row] = -exact;
 }
 
 __global__ __launch_bounds__(256) void bwd_join_dkv_kernel(BwdParams p, bool bias) {
-  const int rows = part_rows(p.n_k), col = 4 * (threadIdx.x & 31);
-  const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
-  if (slot0 >= p.dkv_split.shared()) return;
-  const Place at = place_of(p.dkv_split, bias, p.dkv_split.full + slot0, p.bh, (p.n_k + 127) / 128, false);
-  const int row = at.group * 128 + local;
+  const int rows = part_rows(p.n_k);
+  const PartPlace me = part_place(blockIdx.x * 256 + threadIdx.x, rows);
+  if (me.slot0 >= p.dkv_split.shared()) return;
+  const Place at = place_of(p.dkv_split, bias, p.dkv_split.full + me.slot0, p.bh, (p.n_k + 127) / 128, false);
+  const int row = at.group * 128 + me.row;
   if (row >= p.n_k) return;
-  const size_t out = ((size_t)at.bh * p.n_k + row) * kD + col;
-  store_cols(p.dk + out, sum_parts(p.part_a, p.dkv_split, slot0, rows, local, col), p.scale);
-  store_cols(p.dv + out, sum_parts(p.part_b, p.dkv_split, slot0, rows, local, col), 1.f);
+  const size_t out = ((size_t)at.bh * p.n_k + row) * kD + me.col;
+  store_cols(p.dk + out, sum_parts(p.part_a, p.dkv_split, rows, me), p.scale);
+  store_cols(p.dv + out, sum_parts(p.part_b, p.dkv_split, rows, me), 1.f);
 }
 
 // ---- the bias by distance, and the table's gradient -----------------------------------------

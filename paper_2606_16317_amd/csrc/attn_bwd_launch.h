@@ -62,9 +62,10 @@ struct BwdParams {
   int n_rows;
   // units of the dq and of the dk, dv kernel, and the partial results of units that are shared
   WorkSplit dq_split, dkv_split;
-  float* part_a;           // [slots][min(n, 128)][128]: sums of dS K, later of dS^T Q
+  float* part_a;           // [slots][part_rows(n)][128]: sums of dS K, later of dS^T Q
   float* part_b;           // of P K, later of P^T dO
-  float* part_delta;       // [slots][128]
+  float* part_delta;       // [slots][128]: sums of P dP
+  float* part_prime;       // [shared units][128]: -(dO . O)
   // kBwdMask
   const uint8_t* mask;     // [BH][n_units][n_dec], nonzero: skipped
   int tile_q, tile_k;

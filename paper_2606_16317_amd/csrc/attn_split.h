@@ -70,8 +70,10 @@ inline UnitOrder unit_order(bool bias, bool mask, int bh, long long units) {
   return !bias || (bh % 8 == 0 && units >= 4 * 512) ? kHeadsToXcds : kGroupByGroup;
 }
 
-// Rows of a unit's partial sums.
-__host__ __device__ inline int part_rows(int n) { return n < 128 ? n : 128; }
+// Rows of a slot of partial sums: up to 32, or those of the waves that have any.
+__host__ __device__ inline int part_rows(int n) {
+  return n <= 32 ? n : n < 128 ? (n + 31) / 32 * 32 : 128;
+}
 
 // tiles: what a unit streams, at most.  join: what a part adds to the join, in times of a tile.
 inline WorkSplit make_split(long long units, int tiles, double join, UnitOrder order) {

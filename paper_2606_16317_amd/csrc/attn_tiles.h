@@ -256,14 +256,31 @@ __device__ __forceinline__ void store_row(uint16_t* base, int row, const f32x16 
     }
 }
 
-// Store a^T as one row of partial sums.
-__device__ __forceinline__ void store_part(float* row, const f32x16 (&a)[4], int g) {
+// Partial sums of a wave's 32 rows lie as the lanes hold them: 16 times 1 KiB, one store each.  (By
+// rows, the same stores of 16 bytes in 32 rows cost one head of 2048 rows 2 of 52 us.)  Of fewer
+// rows than 32 in all there are `rows` times 16 bytes twice as often, so that single ones lie
+// together.
+__device__ __forceinline__ void store_part(float* slot, const f32x16 (&a)[4], int rows, int w, int lane) {
+  const int r = lane & 31, n = min(rows, 32);
+  if (r >= n) return;
+  float* part = slot + w * 32 * kD + ((lane >> 5) * n + r) * 4;
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      *reinterpret_cast<f32x4*>(row + 32 * db + 8 * i + 4 * g) =
+      *reinterpret_cast<f32x4*>(part + (4 * db + i) * n * 8) =
           f32x4{a[db][4 * i], a[db][4 * i + 1], a[db][4 * i + 2], a[db][4 * i + 3]};
+}
+
+// What thread `id` of a join has: four columns of a row, at `offset` of each of a shared unit's parts.
+struct PartPlace {
+  int slot0, row, col;   // the unit's first slot, its row (0..127) and the first column
+  size_t offset;
+};
+__device__ __forceinline__ PartPlace part_place(int id, int rows) {   // rows: of a slot, part_rows
+  const int in_slot = id % (rows * (kD / 4)), n = min(rows, 32);
+  const int w = in_slot / (n * 32), in_wave = in_slot % (n * 32);
+  return PartPlace{id / (rows * (kD / 4)), 32 * w + in_wave % n, 4 * (in_wave / n), (size_t)in_slot * 4};
 }
 
 // Store four columns of a row of sums, times m, as bf16.

@@ -235,32 +235,33 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
     }
   }
 
-  if (row >= p.n_q) return;
   const float l = half_sum(rs.l_half);
   if (x >= p.split.full) {
+    if (!own) return;
     const size_t slot = x - p.split.full, local = row - q0;
-    store_part(p.part_o + (slot * part_rows(p.n_q) + local) * kD, o, g);
+    const int rows = part_rows(p.n_q);
+    store_part(p.part_o + slot * rows * kD, o, rows, w, lane);
     if (g == 0) {
       p.part_ml[2 * (128 * slot + local)] = rs.m_ref;
       p.part_ml[2 * (128 * slot + local) + 1] = l;
     }
-  } else {
+  } else if (row < p.n_q) {
     store_row(p.o + qoff, row, o, l > 0.f ? 1.f / l : 0.f, g);
     if (g == 0 && p.lse != nullptr)
       p.lse[(size_t)bh * p.n_q + row] = l > 0.f ? (rs.m_ref + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
   }
 }
 
-// Join the parts of a row: 32 lanes a row, four columns a lane.
+// Join the parts of a row, four columns a thread.
 __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
-  const int rows = part_rows(p.n_q), col = 4 * (threadIdx.x & 31);
-  const int id = blockIdx.x * 8 + (threadIdx.x >> 5), slot0 = id / rows, local = id % rows;
-  if (slot0 >= p.split.shared()) return;
-  const Place at = place_of(p.split, true, p.split.full + slot0, p.bh, (p.n_q + 127) / 128, true);
-  const int row = at.group * 128 + local;
+  const int rows = part_rows(p.n_q);
+  const PartPlace me = part_place(blockIdx.x * 256 + threadIdx.x, rows);
+  if (me.slot0 >= p.split.shared()) return;
+  const Place at = place_of(p.split, true, p.split.full + me.slot0, p.bh, (p.n_q + 127) / 128, true);
+  const int row = at.group * 128 + me.row;
   if (row >= p.n_q) return;
-  const auto slot = [&](int i) { return (size_t)(slot0 + i * p.split.shared()); };
-  const auto ml = [&](int i) { return p.part_ml + 2 * (128 * slot(i) + local); };
+  const auto slot = [&](int i) { return (size_t)(me.slot0 + i * p.split.shared()); };
+  const auto ml = [&](int i) { return p.part_ml + 2 * (128 * slot(i) + me.row); };
   float m = neg_inf();
 #pragma unroll 8
   for (int i = 0; i < p.split.parts; ++i) m = fmaxf(m, ml(i)[0]);
@@ -271,12 +272,12 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
     for (int i = 0; i < p.split.parts; ++i) {
       const float f = exp2_fast(ml(i)[0] - m);
       l = fmaf(f, ml(i)[1], l);
-      const f32x4 z = *reinterpret_cast<const f32x4*>(p.part_o + (slot(i) * rows + local) * kD + col);
+      const f32x4 z = *reinterpret_cast<const f32x4*>(p.part_o + slot(i) * rows * kD + me.offset);
 #pragma unroll
       for (int t = 0; t < 4; ++t) x[t] = fmaf(f, z[t], x[t]);
     }
-  store_cols(p.o + ((size_t)at.bh * p.n_q + row) * kD + col, x, l > 0.f ? 1.f / l : 0.f);
-  if (col == 0 && p.lse != nullptr)
+  store_cols(p.o + ((size_t)at.bh * p.n_q + row) * kD + me.col, x, l > 0.f ? 1.f / l : 0.f);
+  if (me.col == 0 && p.lse != nullptr)
     p.lse[(size_t)at.bh * p.n_q + row] =
         l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
 }

@@ -18,7 +18,7 @@ struct BiasFwdParams {
   BiasParams bias;
   int bh;                  // batches times heads
   WorkSplit split;
-  float* part_o;           // workspace [slots][min(n_q, 128)][128]
+  float* part_o;           // workspace [slots][part_rows(n_q)][128]
   float* part_ml;          // workspace [slots][128][2]: reference maximum (log2) and row sum
 };
 
