@@ -12,6 +12,8 @@
 #include "attn_tiles.h"
 #include "bias_fwd_launch.h"
 
+#include <type_traits>
+
 namespace dsattn {
 namespace {
 
@@ -157,12 +159,13 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
                                fmaf(block_max(s[1]), p.c, tb.flat[1])));
     }
 
-    for (int t = t0; t < t1; ++t) {
-      const int buf = (t - t0) & 1;
+    // Tile t, in buffer BUF: s holds its S, sn receives the next one's.
+    auto step = [&](auto BUF, int t, f32x16 (&s)[2], f32x16 (&sn)[2]) {
+      constexpr int buf = decltype(BUF)::value;
       tiles_ready();
       if (t + 2 < t1) fetch_k(buf, t + 2);
       if (t + 1 < t1) fetch_v(buf ^ 1, t + 1);
-      if (!own) continue;
+      if (!own) return;
 
       if (__ballot(m_hat > rs.m_ref + kRescaleSlack) != 0) {
         const bool need = m_hat > rs.m_ref + kRescaleSlack;
@@ -188,7 +191,6 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
         if (i < 16) return row_operand(ka, InLane{}, (i & 1) * kBlockBytes, i >> 1);
         return col_operand(va, InLane{}, ((i - 16) >> 3) * kBlockBytes, ((i - 16) >> 2) & 1, i & 3);
       };
-      f32x16 sn[2];
       float xs[32];
       bf16x8 pf[4];
       auto prob = [&](int e) {
@@ -230,8 +232,11 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
       m_hat = row_join(maximum(fmaf(block_max(sn[0]), p.c, tb_next.flat[0]),
                                fmaf(block_max(sn[1]), p.c, tb_next.flat[1])));
       tb = tb_next;
-      s[0] = sn[0];
-      s[1] = sn[1];
+    };
+    f32x16 s1[2];   // alternating with s: no copies
+    for (int t = t0; t < t1; t += 2) {
+      step(std::integral_constant<int, 0>{}, t, s, s1);
+      if (t + 1 < t1) step(std::integral_constant<int, 1>{}, t + 1, s1, s);
     }
   }
 
