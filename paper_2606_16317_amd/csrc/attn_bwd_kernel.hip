@@ -165,6 +165,7 @@ struct DkvBias {
 };
 struct DqBias {
   alignas(16) float win[2][kWindow];
+  f32x4 sums[kThreads];   // see flush_sums
   int32_t runs[2][64];
   int ends[2];   // of the open runs, see open_tiles
 };
@@ -533,15 +534,45 @@ struct DqSmem {
 //
 // delta: the sum of P dP over the row, which the loop makes on the way, is exact to 32 bits;
 // dO . O is off by the rounding of o, which matters where one key has most of a row, dS being a
-// small difference there.  So dQ is taken with delta' = dO . O and put right at the end,
-// dQ = scale (sum of P (dP - delta') k - (delta - delta') sum of P k), and the dk, dv kernel gets
-// delta.  The fourth product, sum of P k, is its price: without it, dq and dk were off by 4.5e-3
-// of their norm at N = 32760 instead of 2e-3.
+// small difference there.  So dQ is taken with delta' = dO . O and put right at the end, and the dk,
+// dv kernel gets delta.  A row's dS sum up to zero, so what the rounded P (dP - delta') that went
+// into the products sum up to, r, is their error; taking it back as r P,
+//   dQ = scale (sum of bf16(P (dP - delta')) k - r sum of P k),
+// removes that of delta' and most of the rounding's, which is largest where P is.  The fourth
+// product, sum of P k, is the price: 18.8 instead of 16.1 ms at N = 32760 and 10 heads, for dq off by
+// 2.2e-3 of its norm instead of 4.5e-3 (1.7e-3 is the rounding of the result).
+//
+// With a bias delta is divided by the sum of P, which the LSE's rounding leaves some 1e-7 off one:
+// a row's dS then sum up to zero in the table's gradient, too, whose far buckets add up very many.
+struct RowSums {
+  float pdp = 0.f;   // of P dP
+  float p = 0.f;     // of P (kBwdBias)
+  float ds = 0.f;    // of the rounded P (dP - delta')
+};
+
+// a + b into a, what that rounds off into rest.
+__device__ __forceinline__ void add_exactly(float& a, float& rest, float b) {
+  const float x = a + b, y = x - a;
+  rest += (a - (x - y)) + (b - y);
+  a = x;
+}
+
+// With a bias, the sums of 8 tiles at a time go to a lane's sums in LDS: {pdp, its rest, p, its rest}.
+__device__ __forceinline__ void flush_sums(f32x4& lane_sums, RowSums& sums) {
+  f32x4 x = lane_sums;
+  float pdp = x[0], pdp_rest = x[1], p = x[2], p_rest = x[3];
+  add_exactly(pdp, pdp_rest, sums.pdp);
+  add_exactly(p, p_rest, sums.p);
+  lane_sums = f32x4{pdp, pdp_rest, p, p_rest};
+  sums.pdp = sums.p = 0.f;
+}
+
 template <int MODE, bool TAIL>
 __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint32_t row_at, uint32_t col_at,
                                          const bf16x8 (&qf)[8], const bf16x8 (&gf)[8],
                                          f32x16 (&dq)[4], f32x16 (&pk)[4], float nl, float nd,
-                                         float c, int left, int run, float flat, const float* win, float& delta, float& rest) {
+                                         float c, int left, int run, float flat,
+                                         const float* win, RowSums& sums) {
   const uint32_t k_at = lds_addr(sm.k), v_at = lds_addr(sm.v);
   const uint32_t block = (uint32_t)(buf * kTileElems * 2 + b * 32 * kRowBytes);
   f32x16 s = f32x16{}, dp;
@@ -556,7 +587,12 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       for (int v = 0; v < 16; ++v) s[v] = flat;
     }
   }
-  float sum = 0.f;
+  if constexpr (TAIL) {   // keys past the end
+    const int l = lane_now(), limit = left - 4 * (l >> 5);
+#pragma unroll
+    for (int v = 0; v < 16; ++v)
+      if (27 - back(v) >= limit) s[v] = neg_inf();
+  }
   bf16x8 pf[2], df[2];
   // A operands in the order of their products: S, dP, P K, dQ (eight each)
   auto operand = [&](int i) {
@@ -568,7 +604,8 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
     pf[v >> 3][v & 7] = (__bf16)s[v];
   };
   auto grad = [&](int v) {
-    sum = fmaf(s[v], dp[v], sum);
+    sums.pdp = fmaf(s[v], dp[v], sums.pdp);
+    if constexpr (MODE == kBwdBias) sums.p += s[v];
     df[v >> 3][v & 7] = (__bf16)(s[v] * (dp[v] + nd));
   };
   constexpr int RK = 3;
@@ -589,26 +626,21 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       pk[i & 3] = mfma(x, pf[(i & 7) >> 2], pk[i & 3]);
     else
       dq[i & 3] = mfma(x, df[(i & 7) >> 2], dq[i & 3]);
-    // keys past the end: their rows are zeros, but exp2(-lse) may be infinite
-    if (TAIL && i == 8) {
-      const int l = lane_now();
-#pragma unroll
-      for (int v = 0; v < 16; ++v)
-        if (27 - back(v) + 4 * (l >> 5) >= left) s[v] = neg_inf();
-    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {   // as in dkv_block
       if (i >= 9 && i < 15) prob((i - 9) * 2 + e);
       if (i >= 16 && i < 20 && e < 1) prob(i - 4);
       if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
+    if (i >= 24) {
+      const bf16x8& d = df[(i - 24) >> 2];
+      const int j = 2 * (i & 3);
+      sums.ds = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{d[j], d[j + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f},
+                                                sums.ds, false);
+    }
     sched_fence();
   }
   __builtin_amdgcn_s_setprio(0);
-  // a sum of up to 2^18 block sums: what each addition rounds off is kept beside it
-  const float x = delta + sum, y = x - delta;
-  rest += (delta - (x - y)) + (sum - y);
-  delta = x;
 }
 
 template <int MODE>
@@ -683,14 +715,14 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
     p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
     p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // stays where there is no such row
-    if (x >= p.dq_split.full) p.part_prime[(size_t)(x - p.dq_split.full) * 128 + (row - q0)] = nd;
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
   const bool own = q0 + 32 * w < p.n_q;   // this wave has a query
   uint32_t bits = 0xffu;
   TileRuns tile{};
-  float delta = 0.f, rest = 0.f;
+  RowSums sums;
+  if constexpr (MODE == kBwdBias) sm.side.sums[tid] = f32x4{};   // read by this lane alone
   // Visits i0 .. i1 of the 32-key halves.  A ragged last tile has a copy of the block to itself:
   // masking its keys under a branch in every block took 12 registers, and spilled.
   auto visit_blocks = [&](auto tail, int i0, int i1) {
@@ -714,14 +746,24 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       if (visit)
         dq_block<MODE, decltype(tail)::value>(sm, buf, b, row_at, col_at, qf, gf, dq, pk, nl, nd, p.c,
                                               p.n_k - (n_tiles - 1) * kTile - 32 * b,
-                                              run, b == 0 ? tile.flat[0] : tile.flat[1], win, delta,
-                                              rest);
+                                              run, b == 0 ? tile.flat[0] : tile.flat[1], win, sums);
+      if constexpr (MODE == kBwdBias) {
+        if ((i & 15) == 15) flush_sums(sm.side.sums[64 * w + lane_now()], sums);
+      }
     }
   };
   const bool ragged = count > 0 && p.n_k % kTile != 0 && tile_at(count - 1) == n_tiles - 1;
   visit_blocks(std::false_type{}, 0, ragged ? 2 * count - 2 : 2 * count);
   if (ragged) visit_blocks(std::true_type{}, 2 * count - 2, 2 * count);
-  const float exact = half_sum(delta + rest), off_by = exact + nd;
+  float pdp = sums.pdp, total = 0.f;
+  if constexpr (MODE == kBwdBias) {
+    f32x4& mine = sm.side.sums[64 * w + lane_now()];
+    flush_sums(mine, sums);
+    pdp = mine[0] + mine[1];
+    total = half_sum(mine[2] + mine[3]);
+  }
+  pdp = half_sum(pdp);
+  const float ds = half_sum(sums.ds);
   const int l = lane_now(), half = l >> 5;
   row = q0 + w * 32 + (l & 31);
   if (x >= p.dq_split.full) {
@@ -730,17 +772,23 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       const int rows = part_rows(p.n_q);
       store_part(p.part_a + slot * rows * kD, dq, rows, w, l);
       store_part(p.part_b + slot * rows * kD, pk, rows, w, l);
-      if (half == 0) p.part_delta[slot * 128 + (row - q0)] = exact;
+      float* part = p.part_sums + slot * kPartSums + (row - q0);
+      if (half == 0) {
+        part[0] = pdp;
+        part[128] = ds;
+        if (MODE == kBwdBias) part[256] = total;
+      }
     }
     return;
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-off_by, pk[db][v], dq[db][v]);
+    for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-ds, pk[db][v], dq[db][v]);
   if (row < p.n_q) {
     store_row(p.dq + qoff, row, dq, p.scale, half);
-    if (half == 0) p.neg_delta[(size_t)bh * p.n_rows + row] = -exact;
+    if (half == 0)
+      p.neg_delta[(size_t)bh * p.n_rows + row] = -(MODE == kBwdBias && total > 0.f ? pdp / total : pdp);
   }
 }
 
@@ -765,17 +813,21 @@ __global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias
   const Place at = place_of(p.dq_split, bias, p.dq_split.full + me.slot0, p.bh, (p.n_q + 127) / 128, true);
   const int row = at.group * 128 + me.row;
   if (row >= p.n_q) return;
-  float exact = 0.f;
+  float pdp = 0.f, ds = 0.f, total = 0.f;
 #pragma unroll 8
-  for (int j = 0; j < p.dq_split.parts; ++j)
-    exact += p.part_delta[(size_t)(me.slot0 + j * p.dq_split.shared()) * 128 + me.row];
-  const float off_by = exact + p.part_prime[(size_t)me.slot0 * 128 + me.row];
+  for (int j = 0; j < p.dq_split.parts; ++j) {
+    const float* part = p.part_sums + (size_t)(me.slot0 + j * p.dq_split.shared()) * kPartSums + me.row;
+    pdp += part[0];
+    ds += part[128];
+    if (bias) total += part[256];
+  }
   f32x4 x = sum_parts(p.part_a, p.dq_split, rows, me);
   const f32x4 y = sum_parts(p.part_b, p.dq_split, rows, me);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) x[t] = fmaf(-off_by, y[t], x[t]);
+  for (int t = 0; t < 4; ++t) x[t] = fmaf(-ds, y[t], x[t]);
   store_cols(p.dq + ((size_t)at.bh * p.n_q + row) * kD + me.col, x, p.scale);
-  if (me.col == 0) p.neg_delta[(size_t)at.bh * p.n_rows + row] = -exact;
+  if (me.col == 0)
+    p.neg_delta[(size_t)at.bh * p.n_rows + row] = -(bias && total > 0.f ? pdp / total : pdp);
 }
 
 __global__ __launch_bounds__(256) void bwd_join_dkv_kernel(BwdParams p, bool bias) {

@@ -43,6 +43,8 @@ constexpr int kMaxBuckets = 512;   // what the backward pass keeps of them in LD
 // Fill by_dist and runs.
 hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream);
 
+constexpr int kPartSums = 3 * 128;
+
 struct BwdParams {
   const uint16_t* q;       // bf16 [BH][n_q][128]
   const uint16_t* k;       // bf16 [BH][n_k][128]
@@ -58,14 +60,13 @@ struct BwdParams {
   float scale;
   // workspace, rows padded to n_rows (a multiple of 64)
   float* neg_lse2;         // [BH][n_rows]: -lse * log2(e); -inf for rows that saw no key or do not exist
-  float* neg_delta;        // [BH][n_rows]: -(dO . O), then in bias mode -(sum of P dP)
+  float* neg_delta;        // [BH][n_rows]: -(sum of P dP)
   int n_rows;
   // units of the dq and of the dk, dv kernel, and the partial results of units that are shared
   WorkSplit dq_split, dkv_split;
   float* part_a;           // [slots][part_rows(n)][128]: sums of dS K, later of dS^T Q
   float* part_b;           // of P K, later of P^T dO
-  float* part_delta;       // [slots][128]: sums of P dP
-  float* part_prime;       // [shared units][128]: -(dO . O)
+  float* part_sums;        // [slots][kPartSums]: per row the sums of P dP, of the rounded dS, of P
   // kBwdMask
   const uint8_t* mask;     // [BH][n_units][n_dec], nonzero: skipped
   int tile_q, tile_k;

@@ -802,13 +802,13 @@ size_t bwd_part_bytes(int mode, int bh, int n_q, int n_k) {
                            floats(dsattn::bwd_split(mode, bh, n_k, n_q), n_k)) * sizeof(float));
 }
 
-size_t bwd_delta_bytes(const dsattn::WorkSplit& dq) {
-  return ((size_t)dq.slots() + (size_t)dq.shared()) * 128 * sizeof(float);
+size_t bwd_sums_bytes(const dsattn::WorkSplit& dq) {
+  return (size_t)dq.slots() * dsattn::kPartSums * sizeof(float);
 }
 
 size_t bwd_bytes(int mode, int B, int H, int n_q, int n_k) {
   return bwd_rows_bytes(B, H, n_q) + 2 * bwd_part_bytes(mode, B * H, n_q, n_k) +
-         bwd_delta_bytes(dsattn::bwd_split(mode, B * H, n_q, n_k));
+         bwd_sums_bytes(dsattn::bwd_split(mode, B * H, n_q, n_k));
 }
 
 // What both backward calls fill in alike, n_q and n_k set before.
@@ -821,8 +821,7 @@ void bwd_slices(int mode, dsattn::BwdParams& p, Slices& ws) {
   p.dkv_split = dsattn::bwd_split(mode, p.bh, p.n_k, p.n_q);
   p.part_a = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
   p.part_b = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
-  p.part_delta = static_cast<float*>(ws.take(bwd_delta_bytes(p.dq_split)));
-  p.part_prime = p.part_delta + (size_t)p.dq_split.slots() * 128;
+  p.part_sums = static_cast<float*>(ws.take(bwd_sums_bytes(p.dq_split)));
 }
 
 bool sane_extents(int B, int H, int n) {

@@ -3,9 +3,18 @@ elementwise bounds of what a kernel with bf16 operands and 32-bit sums may be of
 
 Half a step of a rounding is U16 = 2^-8 (bf16) or U32 = 2^-24 of the value.  The kernels round
 P and dS to bf16 for the products, and the results to bf16.  They sum delta in 32 bits; only dq
-begins with the rounded output's delta' and corrects for it afterwards.  Per logit the 32-bit arithmetic is off by at most ETA (128 products
-and their sum, the product with the scale, the difference to the LSE and the LSE's own
-rounding), and exp2 and log2 by a few units in the last place.
+begins with the rounded output's delta' and corrects for it afterwards (see dq below).  Per logit the
+32-bit arithmetic is off by at most ETA (128 products and their sum, the product with the scale, the
+difference to the LSE and the LSE's own rounding), and exp2 and log2 by a few units in the last
+place.
+
+dq = scale (sum D k - r sum Pr k) with D = bf16(P (dP - delta')), r = sum D and Pr = bf16(P).  With
+e = delta - delta' and D = dS + e P + eps, sum dS = 0 and sum P = 1 give r = e + sum eps (and the
+rounding of that sum), so that dq is off by
+    scale (sum eps k - (sum eps) sum Pr k + e sum (P - Pr) k),
+|eps| <= what dk's dS is off by + (half a step) |e| P.  An eps therefore counts with its own key and
+with the row's mean one; most of it cancels (eps is largest where P is), which a bound by absolute
+values does not see.
 """
 
 import math
@@ -65,10 +74,11 @@ class Ref:
         d_prime = ((d_o + 130 * U32 * self.o.abs()) * do.abs()).sum(-1, keepdim=True)
         self.b_ds = 1.01 * (rel * self.ds.abs() + self.p * (d_dp + d_delta + 2 * U32 * (dp.abs() + delta.abs())))
         b_k = self.b_ds + (U16 + n) * self.ds.abs()
-        # dq: the rounding of P (dP - delta') and of P in the correction
+        # dq: eps and e (P - Pr)
         b_q = b_k + 2 * (U16 + n + rel) * self.p * (d_prime + d_delta)
         self.b_dv = U16 * self.dv.abs() + t((U16 + n + rel) * self.p) @ do.abs()
-        self.b_dq = U16 * self.dq.abs() + scale * (b_q @ k.abs())
+        mean_k = self.p @ k.abs()
+        self.b_dq = U16 * self.dq.abs() + scale * (b_q @ k.abs() + 1.01 * b_q.sum(-1, keepdim=True) * mean_k)
         self.b_dk = U16 * self.dk.abs() + scale * (t(b_k) @ q.abs())
 
     def add_table(self, bucket, n_buckets):
