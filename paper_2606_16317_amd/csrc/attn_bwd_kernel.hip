@@ -605,7 +605,6 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
   };
   auto grad = [&](int v) {
     sums.pdp = fmaf(s[v], dp[v], sums.pdp);
-    if constexpr (MODE == kBwdBias) sums.p += s[v];
     df[v >> 3][v & 7] = (__bf16)(s[v] * (dp[v] + nd));
   };
   constexpr int RK = 3;
@@ -633,6 +632,7 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
     if (i >= 24) {
+      if constexpr (MODE == kBwdBias) sums.p += s[2 * (i - 24)] + s[2 * (i - 24) + 1];
       const bf16x8& d = df[(i - 24) >> 2];
       const int j = 2 * (i & 3);
       sums.ds = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{d[j], d[j + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f},
