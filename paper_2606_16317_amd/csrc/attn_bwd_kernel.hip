@@ -532,22 +532,25 @@ struct DqSmem {
 // A workgroup owns 128 queries, a wave 32 of them, and streams the keys in tiles of 64.  Per 32
 // keys: S^T = K Q^T and dP^T = V dO^T with queries as columns, then dQ^T += K^T dS^T.
 //
-// delta: the sum of P dP over the row, which the loop makes on the way, is exact to 32 bits;
-// dO . O is off by the rounding of o, which matters where one key has most of a row, dS being a
-// small difference there.  So dQ is taken with delta' = dO . O and put right at the end, and the dk,
-// dv kernel gets delta.  A row's dS sum up to zero, so what the rounded P (dP - delta') that went
-// into the products sum up to, r, is their error; taking it back as r P,
+// delta: dO . O is off by the rounding of o, which matters where one key has most of a row, dS being
+// a small difference there.  So dQ is taken with delta' = dO . O and put right at the end, and the dk,
+// dv kernel gets delta' + (sum of P (dP - delta')), exact to 32 bits.  (Both kernels begin dP with
+// -delta or nearly that: the matrix unit's rounding leans one way along a sum, the same way then.)
+//
+// A row's dS sum up to zero, so what the rounded P (dP - delta') that went into the products sum up
+// to, r, is their error; taking it back as r P,
 //   dQ = scale (sum of bf16(P (dP - delta')) k - r sum of P k),
 // removes that of delta' and most of the rounding's, which is largest where P is.  The fourth
 // product, sum of P k, is the price: 18.8 instead of 16.1 ms at N = 32760 and 10 heads, for dq off by
-// 2.2e-3 of its norm instead of 4.5e-3 (1.7e-3 is the rounding of the result).
+// 2.1e-3 of its norm instead of 4.5e-3 (1.7e-3 is the rounding of the result).
 //
-// With a bias delta is divided by the sum of P, which the LSE's rounding leaves some 1e-7 off one:
-// a row's dS then sum up to zero in the table's gradient, too, whose far buckets add up very many.
+// With a bias the correction of delta' is divided by the sum of P, which the LSE's rounding leaves
+// some 1e-7 off one, so that a row's dS sum up to zero in the table's gradient, too, whose far
+// buckets add up very many.
 struct RowSums {
-  float pdp = 0.f;   // of P dP
-  float p = 0.f;     // of P (kBwdBias)
-  float ds = 0.f;    // of the rounded P (dP - delta')
+  float ds = 0.f;        // of P (dP - delta')
+  float rounded = 0.f;   // of the same, rounded
+  float p = 0.f;         // of P (kBwdBias)
 };
 
 // a + b into a, what that rounds off into rest.
@@ -557,14 +560,14 @@ __device__ __forceinline__ void add_exactly(float& a, float& rest, float b) {
   a = x;
 }
 
-// With a bias, the sums of 8 tiles at a time go to a lane's sums in LDS: {pdp, its rest, p, its rest}.
+// With a bias, the sums of 8 tiles at a time go to a lane's sums in LDS: {ds, its rest, p, its rest}.
 __device__ __forceinline__ void flush_sums(f32x4& lane_sums, RowSums& sums) {
-  f32x4 x = lane_sums;
-  float pdp = x[0], pdp_rest = x[1], p = x[2], p_rest = x[3];
-  add_exactly(pdp, pdp_rest, sums.pdp);
+  const f32x4 x = lane_sums;
+  float ds = x[0], ds_rest = x[1], p = x[2], p_rest = x[3];
+  add_exactly(ds, ds_rest, sums.ds);
   add_exactly(p, p_rest, sums.p);
-  lane_sums = f32x4{pdp, pdp_rest, p, p_rest};
-  sums.pdp = sums.p = 0.f;
+  lane_sums = f32x4{ds, ds_rest, p, p_rest};
+  sums.ds = sums.p = 0.f;
 }
 
 template <int MODE, bool TAIL>
@@ -593,6 +596,9 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
     for (int v = 0; v < 16; ++v)
       if (27 - back(v) >= limit) s[v] = neg_inf();
   }
+  here(nd);   // (the 16 copies of it are made here, not kept in registers around the loop)
+#pragma unroll
+  for (int v = 0; v < 16; ++v) dp[v] = nd;
   bf16x8 pf[2], df[2];
   // A operands in the order of their products: S, dP, P K, dQ (eight each)
   auto operand = [&](int i) {
@@ -604,8 +610,9 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
     pf[v >> 3][v & 7] = (__bf16)s[v];
   };
   auto grad = [&](int v) {
-    sums.pdp = fmaf(s[v], dp[v], sums.pdp);
-    df[v >> 3][v & 7] = (__bf16)(s[v] * (dp[v] + nd));
+    const float x = s[v] * dp[v];
+    sums.ds += x;
+    df[v >> 3][v & 7] = (__bf16)x;
   };
   constexpr int RK = 3;
   bf16x8 a[RK];
@@ -620,7 +627,7 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
     if (i < 8)
       s = mfma(x, qf[i], s);
     else if (i < 16)
-      dp = mfma(x, gf[i - 8], i == 8 ? f32x16{} : dp);
+      dp = mfma(x, gf[i - 8], dp);
     else if (i < 24)
       pk[i & 3] = mfma(x, pf[(i & 7) >> 2], pk[i & 3]);
     else
@@ -635,8 +642,8 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       if constexpr (MODE == kBwdBias) sums.p += s[2 * (i - 24)] + s[2 * (i - 24) + 1];
       const bf16x8& d = df[(i - 24) >> 2];
       const int j = 2 * (i & 3);
-      sums.ds = __builtin_amdgcn_fdot2_f32_bf16(bf16x2{d[j], d[j + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f},
-                                                sums.ds, false);
+      sums.rounded = __builtin_amdgcn_fdot2_f32_bf16(
+          bf16x2{d[j], d[j + 1]}, bf16x2{(__bf16)1.f, (__bf16)1.f}, sums.rounded, false);
     }
     sched_fence();
   }
@@ -714,7 +721,7 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
     nd = 0.f;   // whatever o and dO hold where there is no key
   if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
     p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
-    p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // stays where there is no such row
+    p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // for the join, and where there is no such row
   }
 #pragma unroll
   for (int db = 0; db < 4; ++db) dq[db] = pk[db] = f32x16{};
@@ -755,15 +762,13 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
   const bool ragged = count > 0 && p.n_k % kTile != 0 && tile_at(count - 1) == n_tiles - 1;
   visit_blocks(std::false_type{}, 0, ragged ? 2 * count - 2 : 2 * count);
   if (ragged) visit_blocks(std::true_type{}, 2 * count - 2, 2 * count);
-  float pdp = sums.pdp, total = 0.f;
   if constexpr (MODE == kBwdBias) {
     f32x4& mine = sm.side.sums[64 * w + lane_now()];
     flush_sums(mine, sums);
-    pdp = mine[0] + mine[1];
-    total = half_sum(mine[2] + mine[3]);
+    sums.ds = mine[0] + mine[1];
+    sums.p = mine[2] + mine[3];
   }
-  pdp = half_sum(pdp);
-  const float ds = half_sum(sums.ds);
+  const float ds = half_sum(sums.ds), rounded = half_sum(sums.rounded), total = half_sum(sums.p);
   const int l = lane_now(), half = l >> 5;
   row = q0 + w * 32 + (l & 31);
   if (x >= p.dq_split.full) {
@@ -774,8 +779,8 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
       store_part(p.part_b + slot * rows * kD, pk, rows, w, l);
       float* part = p.part_sums + slot * kPartSums + (row - q0);
       if (half == 0) {
-        part[0] = pdp;
-        part[128] = ds;
+        part[0] = ds;
+        part[128] = rounded;
         if (MODE == kBwdBias) part[256] = total;
       }
     }
@@ -784,11 +789,11 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
 #pragma unroll
   for (int db = 0; db < 4; ++db)
 #pragma unroll
-    for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-ds, pk[db][v], dq[db][v]);
+    for (int v = 0; v < 16; ++v) dq[db][v] = fmaf(-rounded, pk[db][v], dq[db][v]);
   if (row < p.n_q) {
     store_row(p.dq + qoff, row, dq, p.scale, half);
     if (half == 0)
-      p.neg_delta[(size_t)bh * p.n_rows + row] = -(MODE == kBwdBias && total > 0.f ? pdp / total : pdp);
+      p.neg_delta[(size_t)bh * p.n_rows + row] = nd - (MODE == kBwdBias && total > 0.f ? ds / total : ds);
   }
 }
 
@@ -813,21 +818,21 @@ __global__ __launch_bounds__(256) void bwd_join_dq_kernel(BwdParams p, bool bias
   const Place at = place_of(p.dq_split, bias, p.dq_split.full + me.slot0, p.bh, (p.n_q + 127) / 128, true);
   const int row = at.group * 128 + me.row;
   if (row >= p.n_q) return;
-  float pdp = 0.f, ds = 0.f, total = 0.f;
+  float ds = 0.f, rounded = 0.f, total = 0.f;
 #pragma unroll 8
   for (int j = 0; j < p.dq_split.parts; ++j) {
     const float* part = p.part_sums + (size_t)(me.slot0 + j * p.dq_split.shared()) * kPartSums + me.row;
-    pdp += part[0];
-    ds += part[128];
+    ds += part[0];
+    rounded += part[128];
     if (bias) total += part[256];
   }
   f32x4 x = sum_parts(p.part_a, p.dq_split, rows, me);
   const f32x4 y = sum_parts(p.part_b, p.dq_split, rows, me);
 #pragma unroll
-  for (int t = 0; t < 4; ++t) x[t] = fmaf(-ds, y[t], x[t]);
+  for (int t = 0; t < 4; ++t) x[t] = fmaf(-rounded, y[t], x[t]);
   store_cols(p.dq + ((size_t)at.bh * p.n_q + row) * kD + me.col, x, p.scale);
-  if (me.col == 0)
-    p.neg_delta[(size_t)at.bh * p.n_rows + row] = -(bias && total > 0.f ? pdp / total : pdp);
+  if (me.col == 0)   // the row's only thread that reads -delta' and writes -delta
+    p.neg_delta[(size_t)at.bh * p.n_rows + row] -= bias && total > 0.f ? ds / total : ds;
 }
 
 __global__ __launch_bounds__(256) void bwd_join_dkv_kernel(BwdParams p, bool bias) {

@@ -60,13 +60,13 @@ struct BwdParams {
   float scale;
   // workspace, rows padded to n_rows (a multiple of 64)
   float* neg_lse2;         // [BH][n_rows]: -lse * log2(e); -inf for rows that saw no key or do not exist
-  float* neg_delta;        // [BH][n_rows]: -(sum of P dP)
+  float* neg_delta;        // [BH][n_rows]: -delta
   int n_rows;
   // units of the dq and of the dk, dv kernel, and the partial results of units that are shared
   WorkSplit dq_split, dkv_split;
   float* part_a;           // [slots][part_rows(n)][128]: sums of dS K, later of dS^T Q
   float* part_b;           // of P K, later of P^T dO
-  float* part_sums;        // [slots][kPartSums]: per row the sums of P dP, of the rounded dS, of P
+  float* part_sums;        // [slots][kPartSums]: the sums of a row's RowSums
   // kBwdMask
   const uint8_t* mask;     // [BH][n_units][n_dec], nonzero: skipped
   int tile_q, tile_k;
