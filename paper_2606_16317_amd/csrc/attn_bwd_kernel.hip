@@ -12,8 +12,8 @@
 // Both are bound by MFMA and, equally, by LDS reads (1 KiB of operand per MFMA, the other
 // operand stays in registers).  Instruction order is fixed by fences: operands are read two
 // MFMAs ahead, exponentials run under the dP products, dS under the dV products.
-// N = 32760, 10 heads: 18.8 ms, 730 TFLOP/s of the five products the mathematics needs and
-// 1170 of the eight computed; a large library product reaches 1215 on the same card.
+// N = 32760, 10 heads: 18.6 ms, 737 TFLOP/s of the five products the mathematics needs and
+// 1180 of the eight computed; a large library product reaches 1215 on the same card.
 
 #include "attn_bwd_launch.h"
 #include "attn_tiles.h"
@@ -541,7 +541,7 @@ struct DqSmem {
 // to, r, is their error; taking it back as r P,
 //   dQ = scale (sum of bf16(P (dP - delta')) k - r sum of P k),
 // removes that of delta' and most of the rounding's, which is largest where P is.  The fourth
-// product, sum of P k, is the price: 18.8 instead of 16.1 ms at N = 32760 and 10 heads, for dq off by
+// product, sum of P k, is the price: 18.6 instead of 16.1 ms at N = 32760 and 10 heads, for dq off by
 // 2.1e-3 of its norm instead of 4.5e-3 (1.7e-3 is the rounding of the result).
 //
 // With a bias the correction of delta' is divided by the sum of P, which the LSE's rounding leaves
