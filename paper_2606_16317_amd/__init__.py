@@ -584,6 +584,9 @@ def _like(name, t, ref):
 
     if t is None:
         return torch.empty_like(ref)
+    if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.is_cuda and \
+            t.is_contiguous() and t.shape == ref.shape:
+        return t
     if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
         raise TypeError(f"{name} must be a bfloat16 tensor")
     if not t.is_cuda or not t.is_contiguous() or t.shape != ref.shape:
@@ -613,7 +616,7 @@ def dsattn_attn_bwd(rule, q, k, v, o, lse, do, dq=None, dk=None, dv=None, scale=
     if do is None:
         raise TypeError("do must be a bfloat16 tensor")
     do = _like("do", do, q)
-    dq, dk, dv = (_like(n, t, q) for n, t in (("dq", dq), ("dk", dk), ("dv", dv)))
+    dq, dk, dv = _like("dq", dq, q), _like("dk", dk, q), _like("dv", dv, q)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     ls = _ptr(lse, B * H * N, (torch.float32,), "lse")
     mi = None
@@ -654,6 +657,22 @@ def _bias_shape(q, k, v, table, bucket, n_k):
     """(B, H, n_q, n_k, rows of k, d, n_buckets) of checked arguments."""
     import torch
 
+    # All in order: the common case, in one expression.
+    try:
+        if (q.dtype is k.dtype is v.dtype is torch.bfloat16 and table.dtype is torch.float32
+                and bucket.dtype is torch.int32 and q.is_cuda and k.is_cuda and v.is_cuda
+                and table.is_cuda and bucket.is_cuda and q.is_contiguous() and k.is_contiguous()
+                and v.is_contiguous() and table.is_contiguous() and bucket.is_contiguous()):
+            sq, sk, st = q.shape, k.shape, table.shape
+            if len(sq) == len(sk) == 4 and len(st) == 2 and sk == v.shape and \
+                    sq[0] == sk[0] and sq[1] == sk[1] == st[1] and sq[3] == sk[3]:
+                (B, H, n_q, d), rows = sq, sk[2]
+                n = rows if n_k is None else int(n_k)
+                if 0 <= n <= rows and bucket.numel() >= n_q + n - 1 and all(
+                        isinstance(t, torch.Tensor) for t in (q, k, v, table, bucket)):
+                    return B, H, n_q, n, rows, d, st[0]
+    except AttributeError:
+        pass
     for name, t in (("q", q), ("k", k), ("v", v)):
         if not isinstance(t, torch.Tensor) or t.dtype != torch.bfloat16:
             raise TypeError(f"{name} must be a bfloat16 tensor")
@@ -706,11 +725,11 @@ def dsattn_bias_attn_bwd(q, k, v, table, bucket, o, lse, do, dq=None, dk=None, d
     import torch
 
     B, H, n_q, n_k, _, d, n_buckets = _bias_shape(q, k, v, table, bucket, None)
-    for name, t in (("o", o), ("do", do)):
-        if t is None:
-            raise TypeError(f"{name} must be a bfloat16 tensor")
-        _like(name, t, q)
-    dq, dk, dv = (_like(n, t, x) for n, t, x in (("dq", dq, q), ("dk", dk, k), ("dv", dv, v)))
+    if o is None or do is None:
+        raise TypeError(f"{'o' if o is None else 'do'} must be a bfloat16 tensor")
+    _like("o", o, q)
+    _like("do", do, q)
+    dq, dk, dv = _like("dq", dq, q), _like("dk", dk, k), _like("dv", dv, v)
     if dtable is None:
         dtable = torch.empty_like(table)
     elif dtable.shape != table.shape:

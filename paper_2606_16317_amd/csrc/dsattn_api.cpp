@@ -42,15 +42,19 @@ __attribute__((format(printf, 2, 3))) int fail(int code, const char* fmt, ...) {
 }
 
 // True when `p` is memory the GPU can dereference (device or managed allocation).
-bool is_device_pointer(const void* p) {
-  hipPointerAttribute_t attr;
-  const hipError_t e = hipPointerGetAttributes(&attr, p);
+bool is_device_pointer(const void* p, hipPointerAttribute_t* attr) {
+  const hipError_t e = hipPointerGetAttributes(attr, p);
   if (e != hipSuccess) {
     (void)hipGetLastError();  // clear the sticky-free error state left by the query
     return false;
   }
-  return attr.type == hipMemoryTypeDevice || attr.type == hipMemoryTypeManaged ||
-         attr.type == hipMemoryTypeUnified;
+  return attr->type == hipMemoryTypeDevice || attr->type == hipMemoryTypeManaged ||
+         attr->type == hipMemoryTypeUnified;
+}
+
+bool is_device_pointer(const void* p) {
+  hipPointerAttribute_t attr;
+  return is_device_pointer(p, &attr);
 }
 
 struct Request {
@@ -753,7 +757,7 @@ int check_buffers(const Buffer* b, int n, hipStream_t stream) {
   for (int i = 0; i < n; ++i) {
     if (b[i].p == nullptr) return fail(DSATTN_EINVAL, "%s must be non-null", b[i].name);
     hipPointerAttribute_t attr;
-    if (!is_device_pointer(b[i].p) || hipPointerGetAttributes(&attr, b[i].p) != hipSuccess)
+    if (!is_device_pointer(b[i].p, &attr))
       return fail(DSATTN_EINVAL, "%s is not a device pointer", b[i].name);
     if (attr.type == hipMemoryTypeDevice && dev >= 0 && attr.device != dev)
       return fail(DSATTN_EINVAL, "%s is on device %d, the stream on device %d", b[i].name,
@@ -793,35 +797,37 @@ size_t bwd_rows_bytes(int B, int H, int n) {
   return 2 * round_up((size_t)B * (size_t)H * (size_t)dsattn::bwd_padded_rows(n) * sizeof(float));
 }
 
-// Bytes of one of the two arrays of partial sums; the dq and the dk, dv kernel use them in turn.
-size_t bwd_part_bytes(int mode, int bh, int n_q, int n_k) {
+// Division of a backward pass, and the bytes of its workspace's parts: per-row quantities, one of
+// the two arrays of partial sums (the dq and the dk, dv kernel use them in turn), row sums.
+struct BwdPlan {
+  dsattn::WorkSplit dq, dkv;
+  size_t rows, part, sums;
+  size_t total() const { return rows + 2 * part + sums; }
+};
+
+BwdPlan bwd_plan(int mode, int B, int H, int n_q, int n_k) {
+  BwdPlan plan;
+  plan.dq = dsattn::bwd_split(mode, B * H, n_q, n_k);
+  plan.dkv = n_q == n_k ? plan.dq : dsattn::bwd_split(mode, B * H, n_k, n_q);
   const auto floats = [](const dsattn::WorkSplit& s, int n) {
     return (size_t)s.slots() * (size_t)dsattn::part_rows(n) * kHeadDim;
   };
-  return round_up(std::max(floats(dsattn::bwd_split(mode, bh, n_q, n_k), n_q),
-                           floats(dsattn::bwd_split(mode, bh, n_k, n_q), n_k)) * sizeof(float));
+  plan.rows = bwd_rows_bytes(B, H, n_q);
+  plan.part = round_up(std::max(floats(plan.dq, n_q), floats(plan.dkv, n_k)) * sizeof(float));
+  plan.sums = round_up((size_t)plan.dq.slots() * dsattn::kPartSums * sizeof(float));
+  return plan;
 }
 
-size_t bwd_sums_bytes(const dsattn::WorkSplit& dq) {
-  return (size_t)dq.slots() * dsattn::kPartSums * sizeof(float);
-}
-
-size_t bwd_bytes(int mode, int B, int H, int n_q, int n_k) {
-  return bwd_rows_bytes(B, H, n_q) + 2 * bwd_part_bytes(mode, B * H, n_q, n_k) +
-         bwd_sums_bytes(dsattn::bwd_split(mode, B * H, n_q, n_k));
-}
-
-// What both backward calls fill in alike, n_q and n_k set before.
-void bwd_slices(int mode, dsattn::BwdParams& p, Slices& ws) {
+// What both backward calls fill in alike.
+void bwd_slices(const BwdPlan& plan, dsattn::BwdParams& p, Slices& ws) {
   p.n_rows = dsattn::bwd_padded_rows(p.n_q);
-  const size_t row_bytes = (size_t)p.bh * (size_t)p.n_rows * sizeof(float);
-  p.neg_lse2 = static_cast<float*>(ws.take(row_bytes));
-  p.neg_delta = static_cast<float*>(ws.take(row_bytes));
-  p.dq_split = dsattn::bwd_split(mode, p.bh, p.n_q, p.n_k);
-  p.dkv_split = dsattn::bwd_split(mode, p.bh, p.n_k, p.n_q);
-  p.part_a = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
-  p.part_b = static_cast<float*>(ws.take(bwd_part_bytes(mode, p.bh, p.n_q, p.n_k)));
-  p.part_sums = static_cast<float*>(ws.take(bwd_sums_bytes(p.dq_split)));
+  p.neg_lse2 = static_cast<float*>(ws.take(plan.rows / 2));
+  p.neg_delta = static_cast<float*>(ws.take(plan.rows / 2));
+  p.dq_split = plan.dq;
+  p.dkv_split = plan.dkv;
+  p.part_a = static_cast<float*>(ws.take(plan.part));
+  p.part_b = static_cast<float*>(ws.take(plan.part));
+  p.part_sums = static_cast<float*>(ws.take(plan.sums));
 }
 
 bool sane_extents(int B, int H, int n) {
@@ -833,7 +839,7 @@ bool sane_extents(int B, int H, int n) {
 }  // namespace
 
 size_t dsattn_attn_bwd_workspace_bytes(int B, int H, int N) {
-  return sane_extents(B, H, N) ? bwd_bytes(dsattn::kBwdDense, B, H, N, N) : 0;
+  return sane_extents(B, H, N) ? bwd_plan(dsattn::kBwdDense, B, H, N, N).total() : 0;
 }
 
 int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspace_size) {
@@ -858,7 +864,8 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
     g_last_error.clear();
     return DSATTN_OK;
   }
-  const size_t need = bwd_bytes(mode, a.B, a.H, a.N, a.N);
+  const BwdPlan plan = bwd_plan(mode, a.B, a.H, a.N, a.N);
+  const size_t need = plan.total();
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t rows = (size_t)a.B * (size_t)a.H * (size_t)a.N, wide = rows * kHeadDim * 2;
   const int n_units = (a.N + a.tile_q - 1) / a.tile_q, n_dec = (a.N + a.tile_k - 1) / a.tile_k;
@@ -891,7 +898,7 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
   p.c = (float)((double)a.scale * kLog2e);
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
-  bwd_slices(mode, p, ws);
+  bwd_slices(plan, p, ws);
   p.mask = masked ? a.mask_in : nullptr;
   p.tile_q = a.tile_q;
   p.tile_k = a.tile_k;
@@ -950,17 +957,16 @@ dsattn::BiasParams bias_params(const float* table, const int32_t* bucket, int n_
   return b;
 }
 
-size_t bias_fwd_bytes(int B, int H, int n_q, int n_k) {
-  const size_t slots = (size_t)dsattn::bias_fwd_split(B * H, n_q, n_k).slots();
+size_t bias_fwd_bytes(const dsattn::WorkSplit& split, int H, int n_q, int n_k) {
+  const size_t slots = (size_t)split.slots();
   return bias_layout_bytes(H, n_q, n_k) +
          round_up(slots * (size_t)dsattn::part_rows(n_q) * kHeadDim * sizeof(float)) +
          round_up(slots * 128 * 2 * sizeof(float));
 }
 
-size_t bias_bwd_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
-  const size_t parts = (size_t)dsattn::bwd_split(dsattn::kBwdBias, B * H, n_k, n_q).grid();
-  return bias_layout_bytes(H, n_q, n_k) + bwd_bytes(dsattn::kBwdBias, B, H, n_q, n_k) +
-         round_up(parts * (size_t)n_buckets * sizeof(float));
+size_t bias_bwd_bytes(const BwdPlan& plan, int H, int n_q, int n_k, int n_buckets) {
+  return bias_layout_bytes(H, n_q, n_k) + plan.total() +
+         round_up((size_t)plan.dkv.grid() * (size_t)n_buckets * sizeof(float));
 }
 
 // A workspace is never empty, so that it can always be a buffer of the call.
@@ -970,12 +976,15 @@ size_t at_least_one(size_t bytes) { return bytes > 0 ? bytes : kSliceAlign; }
 
 size_t dsattn_bias_attn_workspace_bytes(int B, int H, int n_q, int n_k) {
   if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, 1, 1.f) != DSATTN_OK) return 0;
-  return B == 0 || H == 0 || n_q == 0 ? 0 : at_least_one(bias_fwd_bytes(B, H, n_q, n_k));
+  if (B == 0 || H == 0 || n_q == 0) return 0;
+  return at_least_one(bias_fwd_bytes(dsattn::bias_fwd_split(B * H, n_q, n_k), H, n_q, n_k));
 }
 
 size_t dsattn_bias_attn_bwd_workspace_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
   if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, n_buckets, 1.f) != DSATTN_OK) return 0;
-  return H == 0 ? 0 : at_least_one(bias_bwd_bytes(B, H, n_q, n_k, n_buckets));
+  if (H == 0) return 0;
+  return at_least_one(
+      bias_bwd_bytes(bwd_plan(dsattn::kBwdBias, B, H, n_q, n_k), H, n_q, n_k, n_buckets));
 }
 
 int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t workspace_size) {
@@ -988,7 +997,8 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
     g_last_error.clear();
     return DSATTN_OK;
   }
-  const size_t need = at_least_one(bias_fwd_bytes(a.B, a.H, a.n_q, a.n_k));
+  const dsattn::WorkSplit split = dsattn::bias_fwd_split((int)bh, a.n_q, a.n_k);
+  const size_t need = at_least_one(bias_fwd_bytes(split, a.H, a.n_q, a.n_k));
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t wide = kHeadDim * 2;
   Buffers bufs;
@@ -1018,7 +1028,7 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
   Slices ws{static_cast<char*>(workspace), 0};
   p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
   p.bh = (int)bh;
-  p.split = dsattn::bias_fwd_split(p.bh, a.n_q, a.n_k);
+  p.split = split;
   const size_t slots = (size_t)p.split.slots();
   p.part_o = static_cast<float*>(
       ws.take(slots * (size_t)dsattn::part_rows(a.n_q) * kHeadDim * sizeof(float)));
@@ -1039,7 +1049,8 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
     return DSATTN_OK;
   }
   const size_t bh = (size_t)a.B * (size_t)a.H;
-  const size_t need = at_least_one(bias_bwd_bytes(a.B, a.H, a.n_q, a.n_k, a.n_buckets));
+  const BwdPlan plan = bwd_plan(dsattn::kBwdBias, a.B, a.H, a.n_q, a.n_k);
+  const size_t need = at_least_one(bias_bwd_bytes(plan, a.H, a.n_q, a.n_k, a.n_buckets));
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   // Without queries the table, dk and dv still get their zeros, without keys dq.
   const size_t wide = kHeadDim * 2, q_rows = bh * (size_t)a.n_q, k_rows = bh * (size_t)a.n_k;
@@ -1082,7 +1093,7 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
   p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
-  bwd_slices(dsattn::kBwdBias, p, ws);
+  bwd_slices(plan, p, ws);
   p.dtable = a.dtable;
   p.dtable_part = static_cast<float*>(
       ws.take((size_t)p.dkv_split.grid() * (size_t)a.n_buckets * sizeof(float)));
