@@ -9,11 +9,12 @@
 // workgroup's part of dQ in memory: 64 KiB of fp32 atomics for each 21 MFLOP, in an order that
 // changes from run to run.  Two kernels' sums are always in the same order.
 //
-// Both are bound by MFMA and, equally, by LDS reads (1 KiB of operand per MFMA, the other
-// operand stays in registers).  Instruction order is fixed by fences: operands are read two
-// MFMAs ahead, exponentials run under the dP products, dS under the dV products.
-// N = 32760, 10 heads: 18.6 ms, 737 TFLOP/s of the five products the mathematics needs and
-// 1180 of the eight computed; a large library product reaches 1215 on the same card.
+// What bounds both is the power that products and LDS reads draw (1 KiB of operand per MFMA, 3/4 in
+// the dq kernel, where two products share an operand: 4 % faster than reading it for each; the other
+// operand stays in registers).  Instruction order is fixed by fences: operands are read two MFMAs
+// ahead, exponentials run under the dP products, dS under the dV products (P K in the dq kernel).
+// N = 32760, 10 heads: 18.0 ms, 763 TFLOP/s of the five products the mathematics needs and
+// 1220 of the eight computed; a large library product reaches 1215 on the same card.
 
 #include "attn_bwd_launch.h"
 #include "attn_tiles.h"
@@ -541,7 +542,7 @@ struct DqSmem {
 // to, r, is their error; taking it back as r P,
 //   dQ = scale (sum of bf16(P (dP - delta')) k - r sum of P k),
 // removes that of delta' and most of the rounding's, which is largest where P is.  The fourth
-// product, sum of P k, is the price: 18.6 instead of 16.1 ms at N = 32760 and 10 heads, for dq off by
+// product, sum of P k, is the price: some 2 of 18 ms at N = 32760 and 10 heads, for dq off by
 // 2.1e-3 of its norm instead of 4.5e-3 (1.7e-3 is the rounding of the result).
 //
 // With a bias the correction of delta' is divided by the sum of P, which the LSE's rounding leaves
@@ -600,7 +601,8 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
 #pragma unroll
   for (int v = 0; v < 16; ++v) dp[v] = nd;
   bf16x8 pf[2], df[2];
-  // A operands in the order of their products: S, dP, P K, dQ (eight each)
+  // A operands: eight of S, eight of dP, and eight that P K and dQ share, read once: those of the
+  // first 16 keys stay for both, those of the others serve two products in a row
   auto operand = [&](int i) {
     if (i < 16) return row_operand(row_at, block, i < 8 ? k_at : v_at, i & 7);
     return col_operand(col_at, block, k_at, (i & 7) >> 2, i & 3);
@@ -612,26 +614,33 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
   auto grad = [&](int v) {
     const float x = s[v] * dp[v];
     sums.ds += x;
+    if constexpr (MODE == kBwdBias) sums.p += s[v];
     df[v >> 3][v & 7] = (__bf16)x;
   };
-  constexpr int RK = 3;
-  bf16x8 a[RK];
+  bf16x8 a[3], first[4], rest[2];
 #pragma unroll
-  for (int i = 0; i < RK - 1; ++i) a[i] = operand(i);
+  for (int i = 0; i < 2; ++i) a[i] = operand(i);
   sched_fence();
   __builtin_amdgcn_s_setprio(1);
 #pragma unroll
   for (int i = 0; i < 32; ++i) {
-    if (i + RK - 1 < 32) a[(i + RK - 1) % RK] = operand(i + RK - 1);
-    const bf16x8& x = a[i % RK];
-    if (i < 8)
-      s = mfma(x, qf[i], s);
-    else if (i < 16)
-      dp = mfma(x, gf[i - 8], dp);
-    else if (i < 24)
-      pk[i & 3] = mfma(x, pf[(i & 7) >> 2], pk[i & 3]);
-    else
-      dq[i & 3] = mfma(x, df[(i & 7) >> 2], dq[i & 3]);
+    // each is read two products ahead
+    if (i < 14) a[(i + 2) % 3] = operand(i + 2);
+    if (i >= 14 && i < 18) first[i - 14] = operand(i + 2);
+    if (i >= 22 && i < 30 && i % 2 == 0) rest[(i - 22) / 2 % 2] = operand(20 + (i - 22) / 2);
+    if (i < 8) {
+      s = mfma(a[i % 3], qf[i], s);
+    } else if (i < 16) {
+      dp = mfma(a[i % 3], gf[i - 8], dp);
+    } else if (i < 20) {
+      pk[i - 16] = mfma(first[i - 16], pf[0], pk[i - 16]);
+    } else if (i < 24) {
+      dq[i - 20] = mfma(first[i - 20], df[0], dq[i - 20]);
+    } else {
+      const int db = (i - 24) / 2;
+      f32x16& to = i % 2 == 0 ? pk[db] : dq[db];
+      to = mfma(rest[db % 2], i % 2 == 0 ? pf[1] : df[1], to);
+    }
 #pragma unroll
     for (int e = 0; e < 2; ++e) {   // as in dkv_block
       if (i >= 9 && i < 15) prob((i - 9) * 2 + e);
@@ -639,7 +648,6 @@ __device__ __forceinline__ void dq_block(DqSmem<MODE>& sm, int buf, int b, uint3
       if (i >= 16 && i < 24) grad((i - 16) * 2 + e);
     }
     if (i >= 24) {
-      if constexpr (MODE == kBwdBias) sums.p += s[2 * (i - 24)] + s[2 * (i - 24) + 1];
       const bf16x8& d = df[(i - 24) >> 2];
       const int j = 2 * (i & 3);
       sums.rounded = __builtin_amdgcn_fdot2_f32_bf16(
