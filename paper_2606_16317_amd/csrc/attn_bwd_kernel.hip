@@ -13,8 +13,8 @@
 // the dq kernel, where two products share an operand: 4 % faster than reading it for each; the other
 // operand stays in registers).  Instruction order is fixed by fences: operands are read two MFMAs
 // ahead, exponentials run under the dP products, dS under the dV products (P K in the dq kernel).
-// N = 32760, 10 heads: 18.0 ms, 763 TFLOP/s of the five products the mathematics needs and
-// 1220 of the eight computed; a large library product reaches 1215 on the same card.
+// N = 32760, 10 heads: 18.0-18.2 ms, 755-763 TFLOP/s of the five products the mathematics needs and
+// 1209-1220 of the eight computed; a large library product reaches 1204-1219 on the same cards.
 
 #include "attn_bwd_launch.h"
 #include "attn_tiles.h"
