@@ -380,7 +380,8 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
  * first n_k <= k_rows rows of every head are keys (a cache with room; k_rows = n_k otherwise; the
  * other rows are not read).  With few queries -- one, when a token at a time is added -- the keys
  * are split over more workgroups and joined in a fixed order.  Extents >= 0, n_q, k_rows <=
- * 8388607, B*H <= 65535, 1 <= n_buckets <= 512, d = 128; n_k = 0 leaves every row without a key.
+ * 8388607, B*H <= 65535, 1 <= n_buckets <= 512, d = 128, scale >= 1e-30; n_k = 0 leaves every row
+ * without a key.
  *
  * The gradients (dsattn_bias_attn_bwd; k_rows = n_k there) are those of dsattn_attn_bwd, with
  * the bias in S, and

@@ -920,6 +920,8 @@ int check_bias_problem(int B, int H, int n_q, int n_k, int k_rows, int d, int n_
   if (k_rows < n_k) return fail(DSATTN_EINVAL, "k_rows must be >= n_k (got %d and %d)", k_rows, n_k);
   if (!(scale > 0.f) || !std::isfinite(scale))
     return fail(DSATTN_EINVAL, "scale must be finite and > 0 (got %g)", (double)scale);
+  if (scale < 1e-30f)   // the kernels add bias / scale to q.k
+    return fail(DSATTN_EINVAL, "scale must be >= 1e-30 with a bias (got %g)", (double)scale);
   if (d != kHeadDim)
     return fail(DSATTN_EUNSUPPORTED, "head dimension %d is not supported (only 128)", d);
   if (n_buckets < 1 || n_buckets > dsattn::kMaxBuckets)

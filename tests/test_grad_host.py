@@ -116,6 +116,7 @@ def bias_call(pkg, backward, **kw):
     (dict(n_q=-1), -1, ">= 0"),
     (dict(n_k=-1), -1, ">= 0"),
     (dict(scale=float("inf")), -1, "scale"),
+    (dict(scale=1e-38), -1, "1e-30"),
     (dict(d=256), -2, "head dimension"),
     (dict(n_buckets=0), -2, "n_buckets"),
     (dict(n_buckets=513), -2, "n_buckets"),
