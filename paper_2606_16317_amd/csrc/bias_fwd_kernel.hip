@@ -289,10 +289,10 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
 
 }  // namespace
 
-// A part's 64 KiB are written and read at about 4.5 TB/s, 0.03 us; a tile takes 2 us.
+// A part's 64 KiB are written and read in about 0.02 us; a tile takes 2 us.
 WorkSplit bias_fwd_split(int bh, int n_q, int n_k) {
   const long long units = (long long)bh * ((n_q + 127) / 128);
-  return make_split(units, (n_k + kTile - 1) / kTile, 0.015 * part_rows(n_q) / 128,
+  return make_split(units, (n_k + kTile - 1) / kTile, 0.010 * part_rows(n_q) / 128,
                     unit_order(true, false, bh, units));
 }
 
