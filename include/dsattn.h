@@ -381,15 +381,16 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
  * other rows are not read).  With few queries -- one, when a token at a time is added -- the keys
  * are split over more workgroups and joined in a fixed order.  Extents >= 0, n_q, k_rows <=
  * 8388607, B*H <= 65535, 1 <= n_buckets <= 512, d = 128, scale >= 1e-30; n_k = 0 leaves every row
- * without a key.
+ * without a key.  k, v, table and bucket are not read, and may be NULL, where n_k = 0.
  *
- * The gradients (dsattn_bias_attn_bwd; k_rows = n_k there) are those of dsattn_attn_bwd, with
+ * The gradients (dsattn_bias_attn_bwd; k_rows = n_k and H <= 65535 there) are those of dsattn_attn_bwd, with
  * the bias in S, and
  *
  *   dtable[i][h] = sum over b and the pairs of bucket i of dS          (float [n_buckets][H])
  *
  * whose sums are kept in 32 bits up to the parts of 128 keys and joined in 64, in a fixed order.
- * dout must be finite too.
+ * dout must be finite too.  With B, n_q or n_k = 0 what is left is written, zeros: dtable, and dq or
+ * dk and dv where they have rows; table, bucket and the arrays without a row may then be NULL.
  *
  * Memory, alignment, overlap, workspace and device rules are those of dsattn_attn_bwd; table,
  * bucket, lse_out / lse and dtable are 4-byte aligned.

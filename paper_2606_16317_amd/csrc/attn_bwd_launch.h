@@ -17,12 +17,18 @@ struct BiasParams {
   const float* table;      // [n_buckets][H]
   const int32_t* bucket;   // [n_dist]: bucket of distance e - (n_q - 1), outside [0, n_buckets): closed
   int n_buckets;
-  int n_dist;              // n_q + n_k - 1
+  int n_dist;              // bias_distances
   float* by_dist;          // workspace [H][dist_stride]: bias / scale by distance, -inf: closed
   int32_t* runs;           // workspace [n_runs]: what 32 distances hold, see below
   int dist_stride;         // floats, a multiple of 32
   int n_runs;              // ceil(n_dist / 32)
 };
+
+// Distances that a problem has: none without a query, a key or a batch.  Then nothing reads the table
+// or the buckets, so these are needed, checked, and laid out, only where there are distances.
+inline int bias_distances(int bh, int n_q, int n_k) {
+  return bh > 0 && n_q > 0 && n_k > 0 ? n_q + n_k - 1 : 0;
+}
 
 // A word of runs: the bucket of 32 distances that share one (kRunClosed: all closed), kRunMixed,
 // or run_step where the first `pos` of them share one and the rest another.
@@ -40,7 +46,7 @@ constexpr int run_pos(int run) { return run >> 20 & 1023; }
 constexpr float kClosedBelow = -30000.f;
 constexpr int kMaxBuckets = 512;   // what the backward pass keeps of them in LDS
 
-// Fill by_dist and runs.
+// Fill by_dist and runs (no launch without distances).
 hipError_t launch_bias_prepare(const BiasParams& b, int H, float scale, hipStream_t stream);
 
 constexpr int kPartSums = 3 * 128;

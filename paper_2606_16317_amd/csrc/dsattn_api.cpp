@@ -935,40 +935,45 @@ int check_bias_problem(int B, int H, int n_q, int n_k, int k_rows, int d, int n_
   return DSATTN_OK;
 }
 
-// Distances of a problem, and the floats per head and words of their layout.
-int bias_dist(int n_q, int n_k) { return n_q > 0 && n_k > 0 ? n_q + n_k - 1 : 0; }
-int bias_stride(int n_q, int n_k) { return (bias_dist(n_q, n_k) + 63) / 64 * 64; }
-int bias_runs(int n_q, int n_k) { return (bias_dist(n_q, n_k) + 31) / 32; }
+// Of the distances of a problem: the floats per head and words of their layout.
+int bias_stride(int n_dist) { return (n_dist + 63) / 64 * 64; }
+int bias_runs(int n_dist) { return (n_dist + 31) / 32; }
 
-size_t bias_layout_bytes(int H, int n_q, int n_k) {
-  return round_up((size_t)H * (size_t)bias_stride(n_q, n_k) * sizeof(float)) +
-         round_up((size_t)bias_runs(n_q, n_k) * sizeof(int32_t));
+size_t bias_layout_bytes(int H, int n_dist) {
+  return round_up((size_t)H * (size_t)bias_stride(n_dist) * sizeof(float)) +
+         round_up((size_t)bias_runs(n_dist) * sizeof(int32_t));
 }
 
 dsattn::BiasParams bias_params(const float* table, const int32_t* bucket, int n_buckets, int H,
-                               int n_q, int n_k, Slices& ws) {
+                               int n_dist, Slices& ws) {
   dsattn::BiasParams b{};
   b.table = table;
   b.bucket = bucket;
   b.n_buckets = n_buckets;
-  b.n_dist = bias_dist(n_q, n_k);
-  b.dist_stride = bias_stride(n_q, n_k);
-  b.n_runs = bias_runs(n_q, n_k);
+  b.n_dist = n_dist;
+  b.dist_stride = bias_stride(n_dist);
+  b.n_runs = bias_runs(n_dist);
   b.by_dist = static_cast<float*>(ws.take((size_t)H * (size_t)b.dist_stride * sizeof(float)));
   b.runs = static_cast<int32_t*>(ws.take((size_t)b.n_runs * sizeof(int32_t)));
   return b;
 }
 
-size_t bias_fwd_bytes(const dsattn::WorkSplit& split, int H, int n_q, int n_k) {
+size_t bias_fwd_bytes(const dsattn::WorkSplit& split, int H, int n_q, int n_dist) {
   const size_t slots = (size_t)split.slots();
-  return bias_layout_bytes(H, n_q, n_k) +
+  return bias_layout_bytes(H, n_dist) +
          round_up(slots * (size_t)dsattn::part_rows(n_q) * kHeadDim * sizeof(float)) +
          round_up(slots * 128 * 2 * sizeof(float));
 }
 
-size_t bias_bwd_bytes(const BwdPlan& plan, int H, int n_q, int n_k, int n_buckets) {
-  return bias_layout_bytes(H, n_q, n_k) + plan.total() +
+size_t bias_bwd_bytes(const BwdPlan& plan, int H, int n_dist, int n_buckets) {
+  return bias_layout_bytes(H, n_dist) + plan.total() +
          round_up((size_t)plan.dkv.grid() * (size_t)n_buckets * sizeof(float));
+}
+
+// Heads of a backward pass, each of which has its row of the launches that make the layout and the
+// table's gradient: also where there is no batch.
+int check_bias_heads(int H) {
+  return H <= 65535 ? DSATTN_OK : fail(DSATTN_EINVAL, "H must be <= 65535 (got %d)", H);
 }
 
 // A workspace is never empty, so that it can always be a buffer of the call.
@@ -979,14 +984,17 @@ size_t at_least_one(size_t bytes) { return bytes > 0 ? bytes : kSliceAlign; }
 size_t dsattn_bias_attn_workspace_bytes(int B, int H, int n_q, int n_k) {
   if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, 1, 1.f) != DSATTN_OK) return 0;
   if (B == 0 || H == 0 || n_q == 0) return 0;
-  return at_least_one(bias_fwd_bytes(dsattn::bias_fwd_split(B * H, n_q, n_k), H, n_q, n_k));
+  return at_least_one(bias_fwd_bytes(dsattn::bias_fwd_split(B * H, n_q, n_k), H, n_q,
+                                     dsattn::bias_distances(B * H, n_q, n_k)));
 }
 
 size_t dsattn_bias_attn_bwd_workspace_bytes(int B, int H, int n_q, int n_k, int n_buckets) {
-  if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, n_buckets, 1.f) != DSATTN_OK) return 0;
+  if (check_bias_problem(B, H, n_q, n_k, n_k, kHeadDim, n_buckets, 1.f) != DSATTN_OK ||
+      check_bias_heads(H) != DSATTN_OK)
+    return 0;
   if (H == 0) return 0;
-  return at_least_one(
-      bias_bwd_bytes(bwd_plan(dsattn::kBwdBias, B, H, n_q, n_k), H, n_q, n_k, n_buckets));
+  return at_least_one(bias_bwd_bytes(bwd_plan(dsattn::kBwdBias, B, H, n_q, n_k), H,
+                                     dsattn::bias_distances(B * H, n_q, n_k), n_buckets));
 }
 
 int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t workspace_size) {
@@ -1000,7 +1008,8 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
     return DSATTN_OK;
   }
   const dsattn::WorkSplit split = dsattn::bias_fwd_split((int)bh, a.n_q, a.n_k);
-  const size_t need = at_least_one(bias_fwd_bytes(split, a.H, a.n_q, a.n_k));
+  const int n_dist = dsattn::bias_distances((int)bh, a.n_q, a.n_k);
+  const size_t need = at_least_one(bias_fwd_bytes(split, a.H, a.n_q, n_dist));
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
   const size_t wide = kHeadDim * 2;
   Buffers bufs;
@@ -1008,11 +1017,11 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
   bufs.add("o", a.o, bh * a.n_q * wide, 16, true);
   bufs.add("workspace", workspace, need, kSliceAlign, true);
   if (a.lse_out != nullptr) bufs.add("lse_out", a.lse_out, bh * a.n_q * 4, 4, true);
-  if (a.n_k > 0) {
+  if (n_dist > 0) {
     bufs.add("k", a.k, bh * a.k_rows * wide, 16, false);
     bufs.add("v", a.v, bh * a.k_rows * wide, 16, false);
     bufs.add("table", a.table, (size_t)a.n_buckets * a.H * 4, 4, false);
-    bufs.add("bucket", a.bucket, (size_t)bias_dist(a.n_q, a.n_k) * 4, 4, false);
+    bufs.add("bucket", a.bucket, (size_t)n_dist * 4, 4, false);
   }
   if ((rc = check_buffers(bufs.b, bufs.n, a.stream)) != DSATTN_OK) return rc;
   dsattn::BiasFwdParams p{};
@@ -1028,7 +1037,7 @@ int dsattn_bias_attn_fwd(const dsattn_bias_args* args, void* workspace, size_t w
   p.c = (float)((double)a.scale * kLog2e);
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
-  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
+  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, n_dist, ws);
   p.bh = (int)bh;
   p.split = split;
   const size_t slots = (size_t)p.split.slots();
@@ -1045,16 +1054,17 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   if (args == nullptr) return fail(DSATTN_EINVAL, "args must be non-null");
   const dsattn_bias_bwd_args& a = *args;
   int rc = check_bias_problem(a.B, a.H, a.n_q, a.n_k, a.n_k, a.d, a.n_buckets, a.scale);
-  if (rc != DSATTN_OK) return rc;
+  if (rc != DSATTN_OK || (rc = check_bias_heads(a.H)) != DSATTN_OK) return rc;
   if (a.H == 0) {
     g_last_error.clear();
     return DSATTN_OK;
   }
   const size_t bh = (size_t)a.B * (size_t)a.H;
   const BwdPlan plan = bwd_plan(dsattn::kBwdBias, a.B, a.H, a.n_q, a.n_k);
-  const size_t need = at_least_one(bias_bwd_bytes(plan, a.H, a.n_q, a.n_k, a.n_buckets));
+  const int n_dist = dsattn::bias_distances((int)bh, a.n_q, a.n_k);
+  const size_t need = at_least_one(bias_bwd_bytes(plan, a.H, n_dist, a.n_buckets));
   if ((rc = check_workspace(workspace, workspace_size, need)) != DSATTN_OK) return rc;
-  // Without queries the table, dk and dv still get their zeros, without keys dq.
+  // Without queries dtable, dk and dv still get their zeros, without keys dq, without a batch dtable.
   const size_t wide = kHeadDim * 2, q_rows = bh * (size_t)a.n_q, k_rows = bh * (size_t)a.n_k;
   Buffers bufs;
   bufs.add("dtable", a.dtable, (size_t)a.n_buckets * a.H * 4, 4, true);
@@ -1072,9 +1082,9 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
     bufs.add("dk", a.dk, k_rows * wide, 16, true);
     bufs.add("dv", a.dv, k_rows * wide, 16, true);
   }
-  if (q_rows > 0 && k_rows > 0) {
+  if (n_dist > 0) {
     bufs.add("table", a.table, (size_t)a.n_buckets * a.H * 4, 4, false);
-    bufs.add("bucket", a.bucket, (size_t)bias_dist(a.n_q, a.n_k) * 4, 4, false);
+    bufs.add("bucket", a.bucket, (size_t)n_dist * 4, 4, false);
   }
   if ((rc = check_buffers(bufs.b, bufs.n, a.stream)) != DSATTN_OK) return rc;
   dsattn::BwdParams p{};
@@ -1094,7 +1104,7 @@ int dsattn_bias_attn_bwd(const dsattn_bias_bwd_args* args, void* workspace, size
   p.c = (float)((double)a.scale * kLog2e);
   p.scale = a.scale;
   Slices ws{static_cast<char*>(workspace), 0};
-  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, a.n_q, a.n_k, ws);
+  p.bias = bias_params(a.table, a.bucket, a.n_buckets, a.H, n_dist, ws);
   bwd_slices(plan, p, ws);
   p.dtable = a.dtable;
   p.dtable_part = static_cast<float*>(

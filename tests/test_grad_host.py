@@ -132,6 +132,26 @@ def test_bias_refusals(backward, kw, rc, message):
     assert message in pkg.last_error()
 
 
+def test_no_batch_lays_nothing_out():
+    """Without a batch no pair exists: neither table nor bucket is needed, and nothing of their
+    layout by distance is planned -- the number of distances decides both."""
+    pkg = _lib()
+    size = pkg.lib().dsattn_bias_attn_bwd_workspace_bytes
+    none = size(0, 2, 0, 0, 8)
+    assert size(0, 2, 5000, 7000, 8) == size(0, 2, 5000, 0, 8) == none
+    assert size(1, 2, 5000, 7000, 8) > none + 2 * 12000 * 4
+
+
+@pytest.mark.parametrize("B", [0, 1])
+def test_bias_gradient_heads(B):
+    """Heads are a dimension of its launches whatever the batch."""
+    pkg = _lib()
+    assert bias_call(pkg, True, B=B, H=70000) == -1
+    assert "65535" in pkg.last_error()
+    assert pkg.lib().dsattn_bias_attn_bwd_workspace_bytes(B, 70000, 64, 64, 8) == 0
+    assert pkg.lib().dsattn_bias_attn_bwd_workspace_bytes(B, 65535, 64, 64, 8) > 0
+
+
 def test_bias_cache_and_empty_problems():
     pkg = _lib()
     assert bias_call(pkg, False, n_k=64, k_rows=63) == -1
