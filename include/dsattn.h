@@ -329,7 +329,8 @@ int dsattn_quantize_mxfp8_shift(const void* src, const float* shift, void* codes
  * 128), whose o and lse_out then belong to it.  The other rules are DSATTN_EUNSUPPORTED: pass
  * the mask that they wrote.  A skipped pair costs nothing where its neighbours in a 64-row tile
  * and 128-row block are skipped too, and contributes to no gradient; a row that kept nothing
- * (lse = -inf) gets dq = 0, a key that no row kept dk = dv = 0.  The output of an MX-FP8 call
+ * (lse = -inf) gets dq = 0, a key that no row kept dk = dv = 0; a row whose LSE is NaN gets
+ * dq = NaN and makes dk and dv of the keys that it kept NaN.  The output of an MX-FP8 call
  * has no backward pass here (its LSE is that of the quantised scores).
  *
  * All arrays as in the forward pass: q, k, v, o, dout, dq, dk, dv contiguous bf16

@@ -723,10 +723,10 @@ __global__ __launch_bounds__(kThreads, 2) void bwd_dq_kernel(BwdParams p) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) nd = fmaf(-(float)of[i][j], (float)gf[i][j], nd);
   nd = half_sum(nd);
-  if (lse > neg_inf())
-    nl = -lse * 1.4426950408889634f;
-  else
+  if (lse == neg_inf())
     nd = 0.f;   // whatever o and dO hold where there is no key
+  else
+    nl = -lse * 1.4426950408889634f;   // (of a NaN the row's probabilities are NaN, too)
   if (p.dq_split.part(x) == 0 && row < p.n_rows && g == 0) {
     p.neg_lse2[(size_t)bh * p.n_rows + row] = nl;
     p.neg_delta[(size_t)bh * p.n_rows + row] = nd;   // for the join, and where there is no such row

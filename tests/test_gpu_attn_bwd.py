@@ -289,3 +289,32 @@ def test_refusals():
                               empty)
     assert all(x.shape == empty.shape for x in out)
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("masked", [False, True])
+def test_a_row_with_a_nan_lse_stays_visible(masked):
+    """A diverged row's LSE makes its dq, and dk and dv of the keys that it kept, NaN."""
+    import paper_2606_16317_amd as dsa
+    from _grad_ref import Ref, random_qkv
+
+    announce(f"NaN LSE masked={masked}")
+    N = 200
+    q, k, v, do = random_qkv(1, 2, N, N, 33)
+    mask = torch.zeros(1, 2, 7, 4, dtype=torch.uint8, device="cuda")
+    mask[0, 1, 2, 3] = 1                        # rows 64 .. 95 do not keep keys 192 .. 199
+    ref = Ref(q, k, v, do)
+    o, lse = ref.o.to(torch.bfloat16), ref.lse.float()
+    kw = dict(tile_q=32, mask_in=mask) if masked else {}
+    rule = dsa.RULE_MASK if masked else dsa.RULE_DENSE
+    first = dsa.dsattn_attn_bwd(rule, q, k, v, o, lse, do, **kw)
+    lse[0, 1, 70] = math.nan
+    dq, dk, dv = dsa.dsattn_attn_bwd(rule, q, k, v, o, lse, do, **kw)
+    assert dq[0, 1, 70].isnan().all()
+    same = torch.ones(1, 2, N, dtype=torch.bool, device="cuda")
+    same[0, 1, 70] = False
+    assert torch.equal(dq[same], first[0][same])
+    kept = 192 if masked else N
+    for x, y in ((dk, first[1]), (dv, first[2])):
+        assert x[0, 1, :kept].isnan().all()
+        assert torch.equal(x[0, 1, kept:], y[0, 1, kept:]) and torch.equal(x[0, 0], y[0, 0])
+    torch.cuda.synchronize()
