@@ -382,7 +382,8 @@ int dsattn_attn_bwd(const dsattn_bwd_args* args, void* workspace, size_t workspa
  * other rows are not read).  With few queries -- one, when a token at a time is added -- the keys
  * are split over more workgroups and joined in a fixed order.  Extents >= 0, n_q, k_rows <=
  * 8388607, B*H <= 65535, 1 <= n_buckets <= 512, d = 128, scale >= 1e-30; n_k = 0 leaves every row
- * without a key.  k, v, table and bucket are not read, and may be NULL, where n_k = 0.
+ * without a key.  k, v, table and bucket are not read, and may be NULL, where n_k = 0.  (A row one of
+ * whose logits is NaN gets NaN, and an LSE of NaN.)
  *
  * The gradients (dsattn_bias_attn_bwd; k_rows = n_k and H <= 65535 there) are those of dsattn_attn_bwd, with
  * the bias in S, and

@@ -66,6 +66,12 @@ __device__ __forceinline__ float row_join(float x) {
   return maximum(__builtin_bit_cast(float, (uint32_t)sw[0]), __builtin_bit_cast(float, (uint32_t)sw[1]));
 }
 
+// LSE (natural) of a row from its reference maximum (log2) and sum; the sum is 0 where it saw no key,
+// NaN where a logit was.
+__device__ __forceinline__ float row_lse(float m, float l) {
+  return l != 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
+}
+
 __device__ __forceinline__ void mask_keys(f32x16 (&s)[2], int lim) {
   here(lim);   // (or the compiler selects in every tile instead of branching in the last)
 #pragma unroll
@@ -253,7 +259,7 @@ __global__ __launch_bounds__(kThreads, 2) void bias_fwd_kernel(BiasFwdParams p) 
   } else if (row < p.n_q) {
     store_row(p.o + qoff, row, o, l > 0.f ? 1.f / l : 0.f, g);
     if (g == 0 && p.lse != nullptr)
-      p.lse[(size_t)bh * p.n_q + row] = l > 0.f ? (rs.m_ref + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
+      p.lse[(size_t)bh * p.n_q + row] = row_lse(rs.m_ref, l);
   }
 }
 
@@ -270,21 +276,22 @@ __global__ __launch_bounds__(256) void bias_join_kernel(BiasFwdParams p) {
   float m = neg_inf();
 #pragma unroll 8
   for (int i = 0; i < p.split.parts; ++i) m = fmaxf(m, ml(i)[0]);
+  // (a part without an open key has the reference -inf and zeros, one of NaN alone the same and NaN,
+  // which the factor 0 leaves)
+  const float ref = m == neg_inf() ? 0.f : m;
   float l = 0.f;
   f32x4 x = f32x4{};
-  if (m > neg_inf())
 #pragma unroll 4
-    for (int i = 0; i < p.split.parts; ++i) {
-      const float f = exp2_fast(ml(i)[0] - m);
-      l = fmaf(f, ml(i)[1], l);
-      const f32x4 z = *reinterpret_cast<const f32x4*>(p.part_o + slot(i) * rows * kD + me.offset);
+  for (int i = 0; i < p.split.parts; ++i) {
+    const float f = exp2_fast(ml(i)[0] - ref);
+    l = fmaf(f, ml(i)[1], l);
+    const f32x4 z = *reinterpret_cast<const f32x4*>(p.part_o + slot(i) * rows * kD + me.offset);
 #pragma unroll
-      for (int t = 0; t < 4; ++t) x[t] = fmaf(f, z[t], x[t]);
-    }
+    for (int t = 0; t < 4; ++t) x[t] = fmaf(f, z[t], x[t]);
+  }
   store_cols(p.o + ((size_t)at.bh * p.n_q + row) * kD + me.col, x, l > 0.f ? 1.f / l : 0.f);
   if (me.col == 0 && p.lse != nullptr)
-    p.lse[(size_t)at.bh * p.n_q + row] =
-        l > 0.f ? (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f : neg_inf();
+    p.lse[(size_t)at.bh * p.n_q + row] = row_lse(ref, l);
 }
 
 }  // namespace

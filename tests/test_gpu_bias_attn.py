@@ -427,3 +427,36 @@ def test_refusals():
     with pytest.raises(ValueError):
         bwd(dtable=table[:-1])
     torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("H,n_q,n_k", [(2, 1, 900), (2, 200, 300), (512, 70, 100)])
+@pytest.mark.parametrize("bad", ["query", "key"])
+def test_a_row_of_nan_logits_stays_visible(H, n_q, n_k, bad):
+    """A NaN query, or an infinite key, makes its rows and their LSE NaN whether their keys are split
+    over workgroups or not, as the softmax does, and from that LSE the gradients; other heads keep
+    their bits."""
+    import paper_2606_16317_amd as dsa
+
+    announce(f"NaN logits by a {bad}, H={H} n_q={n_q} n_k={n_k}")
+    q, k, v, do, table, m, ref = make(1, H, n_q, n_k, "one", 5)
+    first = forward(q, k, v, table, m)
+    grads = dsa.dsattn_bias_attn_bwd(q, k, v, table, m, first["o"], first["lse"], do)
+    row = n_q // 2
+    if bad == "query":
+        q[0, 1, row] = math.nan
+    else:
+        k[0, 1, n_k - 1] = math.inf            # q . k: a sum of infinities of both signs
+    got = forward(q, k, v, table, m)
+    hit = torch.zeros(1, H, n_q, dtype=torch.bool, device="cuda")
+    hit[0, 1, slice(row, row + 1) if bad == "query" else slice(None)] = True
+    assert torch.equal(got["lse"].isnan(), hit)
+    assert torch.equal(got["o"].isnan(), hit[..., None].expand_as(got["o"]))
+    for name, x in got.items():
+        assert torch.equal(x[~hit], first[name][~hit]), name
+    out = dsa.dsattn_bias_attn_bwd(q, k, v, table, m, got["o"], got["lse"], do)
+    assert torch.equal(out[0].isnan(), hit[..., None].expand_as(out[0]))
+    assert all(x[:, 1].isnan().all() for x in out[1:3]) and out[3][0, 1].isnan()
+    others = [h for h in range(H) if h != 1]
+    for x, y in zip(out, grads):
+        assert torch.equal(x[:, others], y[:, others])
+    torch.cuda.synchronize()
