@@ -10,7 +10,8 @@ Tensor conventions: q, k, v, o are contiguous bf16 tensors of shape [B, H, N, 12
 {tiles_total, tiles_skipped, elems_total, elems_skipped} per head); ``mask_out`` is a
 uint8 tensor of B*H*ceil(N/tile_q)*ceil(N/64) elements (tile_q = 128, or 32 for per-wave
 decisions); ``lse_out`` a float32 tensor of
-B*H*N elements.
+B*H*N elements.  Outputs and scratch that are not given come from the pool of the stream that
+the call runs on.
 """
 
 from __future__ import annotations
@@ -264,6 +265,17 @@ def _stream(stream):
         torch.cuda.current_device())
 
 
+def _pool(stream, device):
+    """Context in which torch allocates from the pool of `stream`, and that stream's device
+    (`device` for a stream that does not name its own)."""
+    import torch
+
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream.cuda_stream,
+                                           device=getattr(stream, "device", device))
+    return torch.cuda.stream(stream), stream.device
+
+
 def _workspace(nbytes, device, stream, optional=False):
     """Scratch of one call, from the pool of the stream that the call runs on: once this
     reference is gone, only later work of that stream can get the memory.  (Without `stream`
@@ -280,10 +292,7 @@ def _workspace(nbytes, device, stream, optional=False):
     if stream is None:
         on, device = contextlib.nullcontext(), "cuda"
     else:
-        if not isinstance(stream, torch.cuda.Stream):
-            stream = torch.cuda.ExternalStream(stream.cuda_stream,
-                                               device=getattr(stream, "device", device))
-        on, device = torch.cuda.stream(stream), stream.device
+        on, device = _pool(stream, device)
     with on:
         if not optional:
             return torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -295,10 +304,29 @@ def _workspace(nbytes, device, stream, optional=False):
             return None
 
 
-def _out(q, o):
+def _new(make, device, stream):
+    """Output `make()` of a call on `stream`, from that stream's pool: work of the current stream
+    that is queued already may still use what its own pool would give, and what is dropped before
+    the call has run must not go to the current stream's next allocation.  The current stream, which
+    may wait for `stream` and read the output, is recorded as a user."""
     import torch
 
-    return torch.empty_like(q) if o is None else o
+    with _pool(stream, device)[0]:
+        t = make()
+    here = torch.cuda.current_stream(device)
+    if here.cuda_stream != stream.cuda_stream:
+        t.record_stream(here)
+    return t
+
+
+def _out(q, o, stream):
+    import torch
+
+    if o is not None:
+        return o
+    if stream is None:
+        return torch.empty_like(q)
+    return _new(lambda: torch.empty_like(q), getattr(q, "device", None), stream)
 
 
 def _buffers(B, H, N, stats_out, mask_out=None, lse_out=None, tile_q=TILE_Q, tile_k=TILE_K):
@@ -316,7 +344,7 @@ def _buffers(B, H, N, stats_out, mask_out=None, lse_out=None, tile_q=TILE_Q, til
 def dynsparse_attn_fwd(q, k, v, o=None, scale=None, recall_target=0.95, tile_q=TILE_Q,
                        tile_k=TILE_K, stats_out=None, stream=None):
     """DynSparse forward with lambda = ln((1 - recall_target) / N); returns o."""
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, _, _ = _buffers(B, H, N, stats_out)
@@ -330,7 +358,7 @@ def dynsparse_attn_fwd(q, k, v, o=None, scale=None, recall_target=0.95, tile_q=T
 def dynsparse_attn_fwd_lambda(q, k, v, o=None, scale=None, lam=-6.0, tile_q=TILE_Q,
                               tile_k=TILE_K, stats_out=None, stream=None):
     """DynSparse forward with an explicit threshold lambda (natural log); returns o."""
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, _, _ = _buffers(B, H, N, stats_out)
@@ -344,7 +372,7 @@ def dynsparse_attn_fwd_lambda(q, k, v, o=None, scale=None, lam=-6.0, tile_q=TILE
 def blasst_attn_fwd(q, k, v, o=None, scale=None, threshold=1e-3, tile_q=TILE_Q,
                     tile_k=TILE_K, stats_out=None, stream=None):
     """BLASST-style forward (skip when tile max - running max < ln threshold); returns o."""
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, _, _ = _buffers(B, H, N, stats_out)
@@ -358,7 +386,7 @@ def blasst_attn_fwd(q, k, v, o=None, scale=None, threshold=1e-3, tile_q=TILE_Q,
 def dense_attn_fwd(q, k, v, o=None, scale=None, tile_q=TILE_Q, tile_k=TILE_K,
                    stats_out=None, stream=None):
     """Dense forward of the same kernel family; returns o."""
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, _, _ = _buffers(B, H, N, stats_out)
@@ -376,7 +404,7 @@ def dsattn_attn_fwd_ex(rule, param, q, k, v, o=None, scale=None, tile_q=TILE_Q,
     GPU tensor laid out like ``mask_out``)."""
     import torch
 
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, mk, ls = _buffers(B, H, N, stats_out, mask_out, lse_out, tile_q, tile_k)
@@ -399,7 +427,7 @@ def dsattn_attn_fwd_mxfp8(rule, param, q8, q_scales, k8, k_scales, v, o=None, sc
     [B, H, N, 4], as returned by ``dsattn_quantize_mxfp8``; v is bf16."""
     import torch
 
-    o = torch.empty_like(v) if o is None else o
+    o = _out(v, o, stream)
     B, H, N, d = _shape(v, v, v, o)
     for name, t, n in (("q8", q8, d), ("k8", k8, d), ("q_scales", q_scales, d // 32),
                        ("k_scales", k_scales, d // 32)):
@@ -430,7 +458,7 @@ def dsattn_block_order(grid, block):
     return perm[:n]
 
 
-def _rows(src, index, dst):
+def _rows(src, index, dst, stream):
     import torch
 
     if not isinstance(src, torch.Tensor) or not src.is_cuda or not src.is_contiguous():
@@ -444,7 +472,7 @@ def _rows(src, index, dst):
         raise ValueError(f"index must have N={N} entries (got {index.numel()})")
     row_bytes = int(src.shape[-1]) * src.element_size()
     bh = src.numel() // max(1, N * int(src.shape[-1]))
-    dst = torch.empty_like(src) if dst is None else dst
+    dst = _out(src, dst, stream)
     if dst.shape != src.shape or dst.dtype != src.dtype or not dst.is_contiguous():
         raise ValueError("dst must be a contiguous tensor like src")
     return dst, bh, N, row_bytes
@@ -452,7 +480,7 @@ def _rows(src, index, dst):
 
 def dsattn_gather_rows(src, index, dst=None, stream=None):
     """dst[..., i, :] = src[..., index[i], :] on the GPU; returns dst."""
-    dst, bh, N, row_bytes = _rows(src, index, dst)
+    dst, bh, N, row_bytes = _rows(src, index, dst, stream)
     rc = lib().dsattn_gather_rows(src.data_ptr(), dst.data_ptr(), index.data_ptr(), bh, N,
                                   row_bytes, _stream(stream))
     _check(rc, "dsattn_gather_rows")
@@ -461,7 +489,7 @@ def dsattn_gather_rows(src, index, dst=None, stream=None):
 
 def dsattn_scatter_rows(src, index, dst=None, stream=None):
     """dst[..., index[i], :] = src[..., i, :] on the GPU; returns dst."""
-    dst, bh, N, row_bytes = _rows(src, index, dst)
+    dst, bh, N, row_bytes = _rows(src, index, dst, stream)
     rc = lib().dsattn_scatter_rows(src.data_ptr(), dst.data_ptr(), index.data_ptr(), bh, N,
                                    row_bytes, _stream(stream))
     _check(rc, "dsattn_scatter_rows")
@@ -479,9 +507,12 @@ def dsattn_quantize_mxfp8(x, codes=None, scales=None, shift=None, stream=None):
         raise ValueError("x must be a contiguous bf16 GPU tensor")
     n = int(x.shape[-1])
     rows = x.numel() // max(1, n)
-    codes = torch.empty(x.shape, dtype=torch.uint8, device=x.device) if codes is None else codes
-    if scales is None:
-        scales = torch.empty((*x.shape[:-1], n // 32), dtype=torch.uint8, device=x.device)
+    def new(*shape):
+        make = lambda: torch.empty(shape, dtype=torch.uint8, device=x.device)
+        return make() if stream is None else _new(make, x.device, stream)
+
+    codes = new(*x.shape) if codes is None else codes
+    scales = new(*x.shape[:-1], n // 32) if scales is None else scales
     if shift is None:
         rc = lib().dsattn_quantize_mxfp8(x.data_ptr(), codes.data_ptr(), scales.data_ptr(), rows,
                                          n, _stream(stream))
@@ -506,7 +537,9 @@ def dsattn_key_mean(k, out=None, stream=None):
     if k.dtype != torch.bfloat16 or not k.is_cuda or not k.is_contiguous() or k.dim() != 4:
         raise ValueError("k must be a contiguous bf16 GPU tensor [B, H, N, d]")
     B, H, N, d = (int(x) for x in k.shape)
-    out = torch.empty((B, H, d), dtype=torch.float32, device=k.device) if out is None else out
+    if out is None:
+        make = lambda: torch.empty((B, H, d), dtype=torch.float32, device=k.device)
+        out = make() if stream is None else _new(make, k.device, stream)
     need = lib().dsattn_key_mean_workspace_bytes(B * H, N, d)
     ws = _workspace(need, k.device, stream, optional=True)
     rc = lib().dsattn_key_mean_ws(k.data_ptr(), out.data_ptr(), B * H, N, d,
@@ -529,7 +562,7 @@ def dsattn_attn_fwd_reordered(rule, param, q, k, v, q_index, kv_index, o=None, s
     GPU tensor) is allocated here, from the pool of the call's stream, when not given."""
     import torch
 
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, mk, ls = _buffers(B, H, N, stats_out, mask_out, lse_out, tile_q, tile_k)
@@ -560,7 +593,7 @@ def dsattn_attn_fwd_reordered_noalloc(rule, param, q, k, v, q_index, kv_index, o
     ``o`` (and any optional outputs) to keep this wrapper from allocating either."""
     import torch
 
-    o = _out(q, o)
+    o = _out(q, o, stream)
     B, H, N, d = _shape(q, k, v, o)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     st, mk, ls = _buffers(B, H, N, stats_out, mask_out, lse_out, tile_q, tile_k)
@@ -580,12 +613,13 @@ def dsattn_attn_bwd_workspace_bytes(B, H, N):
     return int(lib().dsattn_attn_bwd_workspace_bytes(B, H, N))
 
 
-def _like(name, t, ref):
-    """t, checked to be a contiguous bf16 GPU tensor of ref's shape; a new one for None."""
+def _like(name, t, ref, stream=None):
+    """t, checked to be a contiguous bf16 GPU tensor of ref's shape; a new one, of a call on
+    `stream`, for None."""
     import torch
 
     if t is None:
-        return torch.empty_like(ref)
+        return _out(ref, t, stream)
     if type(t) is torch.Tensor and t.dtype is torch.bfloat16 and t.is_cuda and \
             t.is_contiguous() and t.shape == ref.shape:
         return t
@@ -618,7 +652,8 @@ def dsattn_attn_bwd(rule, q, k, v, o, lse, do, dq=None, dk=None, dv=None, scale=
     if do is None:
         raise TypeError("do must be a bfloat16 tensor")
     do = _like("do", do, q)
-    dq, dk, dv = _like("dq", dq, q), _like("dk", dk, q), _like("dv", dv, q)
+    dq = _like("dq", dq, q, stream)
+    dk, dv = _like("dk", dk, q, stream), _like("dv", dv, q, stream)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     ls = _ptr(lse, B * H * N, (torch.float32,), "lse")
     mi = None
@@ -711,7 +746,7 @@ def dsattn_bias_attn_fwd(q, k, v, table, bucket, n_k=None, o=None, scale=None, l
     import torch
 
     B, H, n_q, n_k, rows, d, n_buckets = _bias_shape(q, k, v, table, bucket, n_k)
-    o = _like("o", o, q)
+    o = _like("o", o, q, stream)
     scale = 1.0 / math.sqrt(d) if scale is None else scale
     ls = _ptr(lse_out, B * H * n_q, (torch.float32,), "lse_out")
     workspace, at, size = _scratch(workspace, dsattn_bias_attn_workspace_bytes(B, H, n_q, n_k),
@@ -735,9 +770,10 @@ def dsattn_bias_attn_bwd(q, k, v, table, bucket, o, lse, do, dq=None, dk=None, d
         raise TypeError(f"{'o' if o is None else 'do'} must be a bfloat16 tensor")
     _like("o", o, q)
     _like("do", do, q)
-    dq, dk, dv = _like("dq", dq, q), _like("dk", dk, k), _like("dv", dv, v)
+    dq = _like("dq", dq, q, stream)
+    dk, dv = _like("dk", dk, k, stream), _like("dv", dv, v, stream)
     if dtable is None:
-        dtable = torch.empty_like(table)
+        dtable = _out(table, dtable, stream)
     elif dtable.shape != table.shape:
         raise ValueError(f"dtable must have the table's shape {tuple(table.shape)}")
     dt = _ptr(dtable, n_buckets * H, (torch.float32,), "dtable")

@@ -460,3 +460,35 @@ def test_a_row_of_nan_logits_stays_visible(H, n_q, n_k, bad):
     for x, y in zip(out, grads):
         assert torch.equal(x[:, others], y[:, others])
     torch.cuda.synchronize()
+
+
+def test_side_stream_calls_keep_their_outputs():
+    """Outputs that a call on a side stream makes: memory that the current stream allocates and
+    fills right after the call, with the side stream still busy ahead of its kernels, is neither
+    theirs nor, once they are dropped, overwritten by them."""
+    import paper_2606_16317_amd as dsa
+
+    announce("outputs of a side stream")
+    q, k, v, do, table, m, ref = make(1, 2, 300, 300, "both", 6)
+    o, lse = ref.o.to(torch.bfloat16), ref.lse.float()
+    steps = [lambda **kw: (dsa.dsattn_bias_attn_fwd(q, k, v, table, m, **kw),),
+             lambda **kw: dsa.dsattn_bias_attn_bwd(q, k, v, table, m, o, lse, do, **kw),
+             lambda **kw: dsa.dsattn_attn_bwd(dsa.RULE_DENSE, q, k, v, o, lse, do, **kw)]
+    want = [step() for step in steps]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for step, first in zip(steps, want):
+        for drop in (False, True):
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)              # some milliseconds
+            out = step(stream=side)
+            if drop:
+                del out
+            grabbed = [torch.empty_like(x).fill_(7.0) for x in first for _ in range(4)]
+            side.synchronize()
+            torch.cuda.synchronize()
+            assert all((x == 7.0).all() for x in grabbed)
+            if not drop:
+                torch.cuda.current_stream().wait_stream(side)
+                assert all(torch.equal(a, b) for a, b in zip(first, out))
+            del grabbed
