@@ -14,6 +14,8 @@ namespace dsattn {
 //
 // Two workgroups run on each of the 256 CUs at a time, 512 in all, so what is left over after
 // whole rounds of 512 units (all of a small problem) is cut into parts.
+__host__ __device__ constexpr int lesser(int a, int b) { return a < b ? a : b; }
+
 enum UnitOrder { kGroupByGroup, kHeadByHead, kHeadsToXcds };
 struct WorkSplit {
   int units, full, parts;
@@ -22,28 +24,28 @@ struct WorkSplit {
   __host__ __device__ int grid() const { return full + shared() * parts; }
   __host__ __device__ int slots() const { return shared() * parts; }
   // Workgroups go to the 8 XCDs in turn.  kHeadsToXcds: each gets a contiguous share of the units.
-  __device__ int unit(int x) const {
+  __host__ __device__ int unit(int x) const {
     if (x >= full) return full + (x - full) % shared();
     if (order != kHeadsToXcds) return x;
     const int xcd = x & 7;
-    return xcd * (full >> 3) + min(xcd, full & 7) + (x >> 3);
+    return xcd * (full >> 3) + lesser(xcd, full & 7) + (x >> 3);
   }
   // The workgroup that has a unit, or its first part.
-  __device__ int workgroup(int unit) const {
+  __host__ __device__ int workgroup(int unit) const {
     if (unit >= full || order != kHeadsToXcds) return unit;
     const int most = full >> 3, more = full & 7, longer = more * (most + 1);
     const int xcd = unit < longer ? unit / (most + 1) : more + (unit - longer) / most;
-    return 8 * (unit - xcd * most - min(xcd, more)) + xcd;
+    return 8 * (unit - xcd * most - lesser(xcd, more)) + xcd;
   }
-  __device__ int part(int x) const { return x < full ? 0 : (x - full) / shared(); }
+  __host__ __device__ int part(int x) const { return x < full ? 0 : (x - full) / shared(); }
   // This workgroup's share [first, last) of `count` visits.
-  __device__ void share(int x, int count, int& first, int& last) const {
+  __host__ __device__ void share(int x, int count, int& first, int& last) const {
     first = 0;
     last = count;
     if (x < full) return;
     const int n = (count + parts - 1) / parts;
-    first = min(count, part(x) * n);
-    last = min(count, first + n);
+    first = lesser(count, part(x) * n);
+    last = lesser(count, first + n);
   }
 };
 
@@ -53,7 +55,7 @@ struct WorkSplit {
 struct Place {
   int bh, group;
 };
-__device__ inline Place place_of(const WorkSplit& split, bool bias, int unit, int bh, int groups,
+__host__ __device__ inline Place place_of(const WorkSplit& split, bool bias, int unit, int bh, int groups,
                                  bool queries) {
   const bool by_group = split.order == kGroupByGroup;
   const int group = by_group ? unit / bh : unit % groups;

@@ -263,3 +263,20 @@ def test_reference_of_rows_with_nothing():
     assert ref.lse[0, 0, 2] == -float("inf") and not ref.o[0, 0, 2].any()
     assert not ref.dq[0, 0, 2].any() and not ref.ds[0, 0, 2].any()
     assert all(torch.isfinite(x).all() for x in (ref.dq, ref.dk, ref.dv))
+
+
+def test_division_of_work(tmp_path):
+    """Every visit of every unit by one workgroup, in every order (a host program)."""
+    import shutil
+    import subprocess
+
+    if shutil.which("g++") is None or not os.path.exists("/opt/rocm/include/hip/hip_runtime.h"):
+        pytest.skip("no g++ or HIP headers")
+    exe = str(tmp_path / "split_check")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", "-Werror", "-D__HIP_PLATFORM_AMD__",
+                    "-isystem", "/opt/rocm/include",
+                    "-I" + os.path.join(ROOT, "paper_2606_16317_amd", "csrc"),
+                    os.path.join(ROOT, "tests", "c_client", "split_check.cpp"), "-o", exe],
+                   check=True, capture_output=True, text=True)
+    res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert res.stdout == "ok\n" and res.returncode == 0, res.stdout
