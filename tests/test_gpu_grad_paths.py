@@ -1,5 +1,6 @@
 """GPU tests of what only large backward passes and calls of many heads reach: long visit lists of
-masks up to the longest, and units by XCD under a bias."""
+masks up to the longest, units by XCD under a bias, and every block's share of the table's gradient
+of long rows."""
 
 import math
 
@@ -126,3 +127,78 @@ def test_units_by_xcd(B, H, n, kind):
     q, k, v, do, table, m, ref = make(B, H, n, n, kind, H)
     print(ref.check(**forward(q, k, v, table, m)), flush=True)
     print(ref.check(**backward(q, k, v, table, m, ref, do)), flush=True)
+
+
+@pytest.mark.parametrize("kind,n_q,n_k", [("both", 3001, 3001), ("causal", 3001, 3001),
+                                          ("random", 3001, 1600), ("both", 700, 5000)])
+def test_every_block_of_the_table_gradient(kind, n_q, n_k):
+    """One query row a head: the sums have few pairs, so a block that is lost or counted for another
+    bucket shows (test_grad_host.py shows that it would)."""
+    import paper_2606_16317_amd as dsa
+    from _table_case import TableCase
+
+    announce(f"table gradient {kind} n_q={n_q} n_k={n_k}")
+    c = TableCase(kind, n_q, n_k, "cuda")
+    got = dsa.dsattn_bias_attn_bwd(c.q, c.k, c.v, c.table, c.bucket, c.o, c.lse, c.do)
+    print(c.ref.check(dtable=got[3]), flush=True)
+    empty = torch.ones(c.H, n_q, dtype=torch.bool, device="cuda")
+    empty[torch.arange(c.H), c.rows] = False
+    assert not got[0][0][empty].any()
+
+
+def by_distance(x):
+    """Sums of x [R, n] over column - row, from -(R - 1) up."""
+    R, n = x.shape
+    return torch.nn.functional.pad(x.flip(0), (0, R)).flatten()[:R * (n + R - 1)].view(R, -1).sum(0)
+
+
+@pytest.mark.parametrize("n,heads,causal", [(3001, 4, False), (32760, 1, False), (32760, 1, True)])
+def test_table_gradient_of_long_rows_by_norm(n, heads, causal):
+    """Errors of a pair's dS are independent but for a row's (its LSE's rounding, its delta), so in
+    units of 1e-7 of a dS: the logit (128 products in eight steps of sums of some 2 times the logit,
+    and the product with the scale) 7, exp2 1, the LSE's rounding 5, sums of 80 values in 32 bits 3;
+    delta's, 0.3 of it for every pair alike, adds up over the keys that share a row (some 1900 of
+    32760, 175 of 3001: e^(-s^2) of them for logits of deviation s = 1.7) and counts with the root of
+    their number: 3 and 10.  All in one direction: 26e-7.
+
+    The errors e x of independent terms x add up to e times the root of the sum of x^2, whatever the
+    terms themselves add up to: where the two far buckets have nearly all of a row, whose dS sum up
+    to zero, the gradient is a small difference (7.0 where that root is 43.9, in the third head of
+    3001 rows), and an error of 5e-7 of the root is 33e-7 of the gradient.  So the root is what the
+    norm of the error is held against."""
+    import paper_2606_16317_amd as dsa
+    from _grad_ref import random_qkv
+
+    announce(f"table gradient by norm n={n} causal={causal}")
+    nb = 32
+    q, k, v, do = random_qkv(1, heads, n, n, 6)
+    bucket = torch.from_numpy(dsa.dsattn_relative_buckets(n, n, nb, 4096 if causal else 128,
+                                                          causal=causal)).cuda()
+    table = torch.randn(nb, heads, generator=torch.Generator().manual_seed(9)).cuda()
+    o, lse = torch.empty_like(q), torch.empty(1, heads, n, device="cuda")
+    want, square = (torch.zeros(nb + 1, heads, dtype=torch.float64, device="cuda") for _ in range(2))
+    index = torch.where(bucket < 0, nb, bucket).long()
+    j = torch.arange(n, device="cuda")
+    for h in range(heads):
+        bias = torch.cat([table[:, h].double(), torch.full((1,), -math.inf, device="cuda").double()])
+        bias = bias[index]
+        kt, vt = (x[0, h].double().t().contiguous() for x in (k, v))
+        sums = torch.zeros(2, 2 * n - 1, dtype=torch.float64, device="cuda")
+        for lo in range(0, n, 2048):
+            hi = min(n, lo + 2048)
+            i = torch.arange(lo, hi, device="cuda")
+            s = q[0, h, i].double() @ kt / math.sqrt(128) + bias[j[None] - i[:, None] + n - 1]
+            row = torch.logsumexp(s, 1)
+            p = torch.exp(s - row[:, None])
+            oi = p @ v[0, h].double()
+            g = do[0, h, i].double()
+            ds = p * (g @ vt - (g * oi).sum(1, keepdim=True))
+            sums[0, n - hi:2 * n - 1 - lo] += by_distance(ds)
+            sums[1, n - hi:2 * n - 1 - lo] += by_distance(ds * ds)
+            o[0, h, i], lse[0, h, i] = oi.to(torch.bfloat16), row.float()
+        want[:, h].index_add_(0, index, sums[0])
+        square[:, h].index_add_(0, index, sums[1])
+    got = dsa.dsattn_bias_attn_bwd(q, k, v, table, bucket, o, lse, do)[3].double()
+    off, root = (got - want[:nb]).norm(dim=0), square[:nb].sum(0).sqrt()
+    print((off / root).tolist(), (off / want[:nb].norm(dim=0)).tolist(), flush=True)
+    assert (off / root).max().item() <= 3e-6

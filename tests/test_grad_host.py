@@ -280,3 +280,29 @@ def test_division_of_work(tmp_path):
                    check=True, capture_output=True, text=True)
     res = subprocess.run([exe], capture_output=True, text=True, timeout=120)
     assert res.stdout == "ok\n" and res.returncode == 0, res.stdout
+
+
+@pytest.mark.parametrize("kind,n_q,n_k", [("both", 3001, 3001), ("causal", 3001, 3001),
+                                          ("random", 3001, 1600), ("both", 700, 5000)])
+def test_the_table_check_misses_no_block(kind, n_q, n_k):
+    """In the GPU test of these cases any one block of 32 keys that is left out of the table's
+    gradient, or counted twice, exceeds the bound of a bucket; and so does every part of one that goes
+    to the next bucket."""
+    torch = pytest.importorskip("torch")
+    _lib()
+    from _table_case import TableCase
+
+    c = TableCase(kind, n_q, n_k, "cpu")
+    closed = c.at < 0
+    ds = c.ref.ds[0, :, 0].masked_fill(closed, 0.0)                     # [H, n_k]
+    n_b = -(-n_k // 32)
+    block = torch.arange(n_k) // 32
+    part = torch.zeros(c.H, n_b * c.nb, dtype=torch.float64).scatter_add_(
+        1, block[None] * c.nb + c.at.clamp(min=0), ds).view(c.H, n_b, c.nb)
+    bound = 1.02 * c.ref.b_dtable.t()[:, None]                          # [H, 1, nb]
+    open_ = torch.zeros(c.H, n_b).scatter_add_(1, block.expand(c.H, -1), (~closed).float()) > 0
+    seen = (part.abs() > bound).any(-1)
+    assert open_.any() and seen[open_].all()
+    there = part != 0
+    moved = (part.abs() > bound) | (part.abs() > bound.roll(-1, -1))
+    assert moved[there].all()
