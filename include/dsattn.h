@@ -340,8 +340,8 @@ int dsattn_quantize_mxfp8_shift(const void* src, const float* shift, void* codes
  *
  * workspace is a caller-owned device buffer of at least dsattn_attn_bwd_workspace_bytes(B, H, N)
  * bytes (8 a row, and up to 130 MiB of partial sums where the work is cut into parts), 256-byte
- * aligned, overlapping no other buffer of the call; its contents are overwritten.  Every buffer must live on the device of `stream` (the current one for the null
- * stream).
+ * aligned, overlapping no other buffer of the call; its contents are overwritten.  Every buffer
+ * must live on the device of `stream` (the current one for the null stream).
  */
 typedef struct dsattn_bwd_args {
   int rule;              /* DSATTN_RULE_DENSE or DSATTN_RULE_MASK */

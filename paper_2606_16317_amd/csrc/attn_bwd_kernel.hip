@@ -9,12 +9,17 @@
 // workgroup's part of dQ in memory: 64 KiB of fp32 atomics for each 21 MFLOP, in an order that
 // changes from run to run.  Two kernels' sums are always in the same order.
 //
-// What bounds both is the power that products and LDS reads draw (1 KiB of operand per MFMA, 3/4 in
-// the dq kernel, where two products share an operand: 4 % faster than reading it for each; the other
-// operand stays in registers).  Instruction order is fixed by fences: operands are read two MFMAs
-// ahead, exponentials run under the dP products, dS under the dV products (P K in the dq kernel).
-// N = 32760, 10 heads: 18.0-18.2 ms, 755-763 TFLOP/s of the five products the mathematics needs and
-// 1209-1220 of the eight computed; a large library product reaches 1204-1219 on the same cards.
+// The dense kernels run their products at the rate of a large library product, so what bounds them is
+// the power that products and LDS reads draw (1 KiB of operand per MFMA, 3/4 in the dq kernel, where
+// two products share an operand: 4 % faster than reading it for each; the other operand stays in
+// registers).  Instruction order is fixed by fences: operands are read two MFMAs ahead, exponentials
+// run under the dP products, dS under the dV products (P K in the dq kernel).
+// N = 32760, 10 heads: 18.1-18.3 ms, 750-759 TFLOP/s of the five products the mathematics needs and
+// 1200-1215 of the eight computed; a large library product reached 1209-1223 on the same card.
+// The dk, dv kernel's loops hold more waits than they need: its own rows, loaded before the loop, count
+// as pending at every entry, so a block's first products wait for the next tile's loads; and without
+// a bias its tile offset is spilled and read back before each tile's loads.  Its waves wait on 32 % of
+// their cycles, those of the dq kernel on 19 %.
 
 #include "attn_bwd_launch.h"
 #include "attn_tiles.h"

@@ -63,10 +63,12 @@ __host__ __device__ inline Place place_of(const WorkSplit& split, bool bias, int
 }
 
 // Workgroups that run on an XCD at a time stream the same head through its L2 where each XCD has a
-// share of heads (24 heads of 27280 rows forward with a bias 9.14 ms instead of 9.45, 10 of 32760
-// backward 18.78 instead of 18.84), which needs equal shares: not under a mask, whose heads keep
-// more or less, nor where a causal bias leaves a part of a head more than another (5 heads of 32760
-// backward 6.87 ms instead of 5.39, group by group).  Few rounds want the groups in order, too.
+// share of heads (24 heads of 27280 rows forward with a bias 8.69 ms instead of 8.98 group by group;
+// without one, backward, 256 of 1024 0.556 ms instead of 0.583 head by head, 40 of 7800 4.29 instead
+// of 4.32, and from 16 of 32760 to 128 of 4096 the same within 0.3 %), which needs equal shares: not
+// under a mask, whose heads keep more or less, nor where a causal bias leaves a part of a head more
+// than another (5 heads of 32760 backward 6.86 ms instead of 5.37, group by group).  Few rounds want
+// the groups in order, too.
 inline UnitOrder unit_order(bool bias, bool mask, int bh, long long units) {
   if (mask) return kHeadByHead;
   return !bias || (bh % 8 == 0 && units >= 4 * 512) ? kHeadsToXcds : kGroupByGroup;
@@ -78,9 +80,9 @@ __host__ __device__ inline int part_rows(int n) {
 }
 
 // tiles: what a unit streams, at most.  join: what a part adds to the join, in times of a tile.
-// Measured, in parts of the keys or queries: one head of 2048 rows backward 149 us alone, 67 in 4, 54 in
-// the 8 taken here, 57 in 16; one token over 32760 keys of one head 637 us alone, 52 in 16, 30 in 64
-// (86 are taken), 48 in 256.
+// Measured, in parts of the keys or queries: one head of 2048 rows backward 139 us alone, 60 in 4, 50 in
+// the 8 taken here, 53 in 16; one token over 32760 keys of one head 636 us alone, 51 in 16, 29 in 64,
+// 30 in the 86 taken, 47 in 256.
 inline WorkSplit make_split(long long units, int tiles, double join, UnitOrder order) {
   const int rest = (int)(units % 512);
   // Up to 256 workgroups have a CU each and take 0.6 of the time of two on one; a part begins

@@ -8,6 +8,12 @@
 // (one value per head and distance).  A 32 x 32 block whose distances share a bucket, as nearly
 // all do when buckets widen with the distance, adds that one number to the row's reference
 // maximum; only mixed blocks read single values, as the first accumulator of S.
+//
+// 24 heads of 27280 rows: 8.64-8.67 ms, 1050 TFLOP/s, where the dense kernel takes 8.25.  The loop waits
+// for its own prefetch: the query rows, loaded before it, count as pending at every entry, so each
+// step's first products wait for the loads just issued.  Waves wait on 28 % of their cycles (21 % in
+// the dense kernel), the matrix pipes are busy on 57 % (70 %); the core clock, 1.57 GHz against 1.55,
+// makes up for little of it.
 
 #include "attn_tiles.h"
 #include "bias_fwd_launch.h"
